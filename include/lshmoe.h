@@ -15,6 +15,11 @@
  *   lshmoe_decompress_backward, lshmoe_compress_backward   gradients through the two calls above
  *   lshmoe_decompress_combine_backward                      gradients of the fused combine (gate weights and rows)
  *   lshmoe_compress_static      lshmoe_compress on scratch memory built into the library (allocates nothing)
+ *   lshmoe_gate_topk, lshmoe_gate_topk_backward   a token's k experts and their weights from the gate's logits (Eq. 1, Eq. 2)
+ *   lshmoe_expert_forward                         the experts' products on rows grouped by expert (E_i of Eq. 2)
+ *   lshmoe_expert_backward_input, lshmoe_expert_backward_weight   gradients of those products
+ *   lshmoe_mx4_quantize, lshmoe_mx4_dequantize    rows in microscaled 4-bit floating point, and back
+ *   lshmoe_expert_forward_mx4                     the experts' products on such rows and weights
  *
  * Notation: T tokens of dimension d; every token is routed to k distinct
  * experts out of E (assignment a = t*k + j is token t's j-th expert, N = T*k
@@ -83,6 +88,21 @@ enum {
   LSHMOE_FLAG_NO_RESIDUAL = 1u
 };
 
+/* Flags of lshmoe_gate_topk and its backward. */
+enum {
+  /* Weights are the chosen experts' shares of the softmax over all E logits;
+   * without the flag the softmax is over the k chosen ones and they sum to 1. */
+  LSHMOE_FLAG_GATE_FULL_SOFTMAX = 2u
+};
+
+/* Activation behind an expert's product. */
+typedef enum {
+  LSHMOE_ACT_NONE = 0,
+  LSHMOE_ACT_RELU = 1,        /* max(v, 0); slope 0 at 0                                           */
+  LSHMOE_ACT_GELU = 2,        /* v * Phi(v), Phi the normal distribution function (no approximation) */
+  LSHMOE_ACT_INT_RANGE_ = 0x7fffffff /* not an activation: makes every int a representable value, as for lshmoe_dtype */
+} lshmoe_activation;
+
 /* Static, never-freed name of a status code. */
 const char* lshmoe_status_string(int status);
 
@@ -90,7 +110,7 @@ const char* lshmoe_status_string(int status);
  * Valid until the next library call on that thread. */
 const char* lshmoe_last_error(void);
 
-/* ABI version of this header (bumped when a signature changes). */
+/* ABI version of this header (bumped when a signature changes or entry points are added). */
 int lshmoe_abi_version(void);
 
 /*
@@ -389,6 +409,159 @@ lshmoe_status lshmoe_compress_backward(const void* grad_out, const void* grad_ce
                                        const int32_t* seg_of, const int32_t* seg_offsets,
                                        int64_t T, int32_t d, int32_t k, lshmoe_dtype dtype, uint32_t flags,
                                        void* grad_tokens, void* stream);
+
+/*
+ * Choice of the experts (the gating network of Section 2.1, Eq. 1, behind its projection): expert[t][0..k-1] are the
+ * indices of the k largest of logits[t][0..E-1], largest first, the lower index first among equal values, and
+ *     gate_weight[t][j] = exp(l_j - m) / sum exp(l_i - m),    m the largest logit of the token,
+ * the sum over the k chosen logits, or over all E with LSHMOE_FLAG_GATE_FULL_SOFTMAX.  Everything is binary32.
+ * A logit of -inf takes an expert out: it is chosen only when fewer than k others are left, with weight 0.  A token
+ * all of whose logits are -inf gets the experts 0 .. k-1, all with weight 0.  A NaN counts as larger than every number;
+ * the weights of a token that has a NaN or +inf among the logits summed over are NaN, its experts are still k
+ * distinct ones.
+ *
+ *   logits      [T, E]  in   binary32 (as lshmoe_hash_gate writes them)
+ *   expert      [T, k]  out  int32; what lshmoe_compress takes
+ *   gate_weight [T, k]  out  binary32; what lshmoe_decompress_combine takes
+ *
+ * Errors: NULL pointer; T, E, k <= 0; k > E (SHAPE); E > 1024, k > 64, T >= 2^30, unknown flag bits or a pointer that is
+ * not 16-byte aligned (UNSUPPORTED); launch failure (HIP).
+ */
+lshmoe_status lshmoe_gate_topk(const float* logits, int64_t T, int32_t E, int32_t k, uint32_t flags,
+                               int32_t* expert, float* gate_weight, void* stream);
+
+/*
+ * Gradient of the gate's logits with the choice held fixed.  With w = gate_weight[t], g = grad_gate_weight[t] and
+ * h = sum_j w_j g_j:
+ *     grad_logits[t][expert[t][j]] = w_j (g_j - h), 0 for the experts that were not chosen;
+ * with LSHMOE_FLAG_GATE_FULL_SOFTMAX, p the softmax over all E logits (computed again from them):
+ *     grad_logits[t][e] = p_e ((g_j if e is expert[t][j], else 0) - h).
+ * A token all of whose logits are -inf gets a gradient of 0.
+ *
+ *   logits           [T, E]  in   binary32; may be NULL without LSHMOE_FLAG_GATE_FULL_SOFTMAX (not read then)
+ *   expert           [T, k]  in   int32, as written by lshmoe_gate_topk (an id out of range counts as E - 1)
+ *   gate_weight      [T, k]  in   binary32, as written by lshmoe_gate_topk
+ *   grad_gate_weight [T, k]  in   binary32, as written by lshmoe_decompress_combine_backward
+ *   grad_logits      [T, E]  out  binary32; every entry is written
+ *
+ * Errors: as for lshmoe_gate_topk.
+ */
+lshmoe_status lshmoe_gate_topk_backward(const float* logits, const int32_t* expert, const float* gate_weight,
+                                        const float* grad_gate_weight, int64_t T, int32_t E, int32_t k, uint32_t flags,
+                                        float* grad_logits, void* stream);
+
+/*
+ * The experts' products (the linear maps of E_i in Eq. 2) on rows grouped by expert, as lshmoe_compress leaves its
+ * centroids: rows expert_offsets[e] .. expert_offsets[e+1] - 1 belong to expert e, and
+ *     pre[s, :] = W_e x[s, :] + b_e,      out[s, :] = act(pre[s, :]).
+ * Two calls, the first with an activation, are an expert network of two layers.  The number of rows of an expert is
+ * known to the device only and may be 0; rows from expert_offsets[E] on are not read and not written.  Products are
+ * accumulated in binary32, in an order that depends on the sizes only; the activation takes the binary32 value, and pre
+ * and out are rounded once each.
+ *
+ *   x              [rows, d_in]       in   dtype
+ *   w              [E, d_out, d_in]   in   dtype
+ *   bias           [E, d_out]         in   dtype, or NULL
+ *   expert_offsets [E+1]              in   int32, ascending, expert_offsets[0] = 0 (as written by lshmoe_compress);
+ *                                     a value outside 0 .. rows counts as the nearest of the two
+ *   pre            [rows, d_out]      out  dtype, or NULL: the values before the activation, for the backward pass
+ *   out            [rows, d_out]      out  dtype
+ *
+ * Errors: NULL pointer (bias and pre excepted); rows, d_in, d_out, E <= 0 (SHAPE); unknown dtype or activation,
+ * row sizes that are not multiples of 16 bytes, rows >= 2^30, E > 4096, rows of 8 MiB or more, weights of
+ * one expert of 2 GiB or more, more than about 64 GiB of rows, a pointer that is not 16-byte aligned (UNSUPPORTED); launch
+ * failure (HIP).
+ */
+lshmoe_status lshmoe_expert_forward(const void* x, const void* w, const void* bias, const int32_t* expert_offsets,
+                                    int64_t rows, int32_t d_in, int32_t d_out, int32_t E, lshmoe_dtype dtype,
+                                    lshmoe_activation act, void* pre, void* out, void* stream);
+
+/*
+ * Gradient of lshmoe_expert_forward's x, through the activation that made x where there is one:
+ *     grad_x[s, :] = (W_e^T grad_out[s, :]) * act'(pre[s, :]),
+ * grad_out being the gradient of the product W_e x + b_e and pre the values that the layer below stored: x = act(pre).
+ * With LSHMOE_ACT_NONE the factor is 1 and pre is not read (it may be NULL): grad_x is then the gradient of x itself.
+ * Rows from expert_offsets[E] on are not read and not written.
+ *
+ *   grad_out [rows, d_out]  in   dtype
+ *   pre      [rows, d_in]   in   dtype, or NULL with LSHMOE_ACT_NONE
+ *   grad_x   [rows, d_in]   out  dtype
+ *   other arguments as for lshmoe_expert_forward.
+ *
+ * Errors: as for lshmoe_expert_forward; pre NULL with an activation (NULL).
+ */
+lshmoe_status lshmoe_expert_backward_input(const void* grad_out, const void* w, const int32_t* expert_offsets,
+                                           int64_t rows, int32_t d_in, int32_t d_out, int32_t E, lshmoe_dtype dtype,
+                                           lshmoe_activation act, const void* pre, void* grad_x, void* stream);
+
+/*
+ * Bytes of device scratch lshmoe_expert_backward_weight needs for these sizes (host only; may be 0).  Errors: NULL out_bytes;
+ * sizes as for lshmoe_expert_forward.
+ */
+lshmoe_status lshmoe_expert_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t E, lshmoe_dtype dtype,
+                                            size_t* out_bytes);
+
+/*
+ * Gradients of lshmoe_expert_forward's weights and biases, sums over the rows s of expert e:
+ *     grad_w[e] = sum_s grad_out[s, :] (x) x[s, :],      grad_bias[e] = sum_s grad_out[s, :],
+ * accumulated in binary32 in an order that depends on the sizes and offsets only, rounded once.  An expert without rows
+ * gets zeros: every entry of grad_w and grad_bias is written.
+ *
+ *   grad_out  [rows, d_out]     in   dtype; the gradient of W_e x + b_e
+ *   x         [rows, d_in]      in   dtype
+ *   grad_w    [E, d_out, d_in]  out  dtype
+ *   grad_bias [E, d_out]        out  dtype, or NULL
+ *   workspace                   scratch of at least lshmoe_expert_workspace_bytes(...) bytes, 256-byte aligned; contents on
+ *                               entry are ignored.  Calls that may overlap need one each.  May be NULL if 0 bytes are needed
+ *   other arguments as for lshmoe_expert_forward.
+ *
+ * Errors: as for lshmoe_expert_forward (grad_bias may be NULL); workspace too small or misaligned (WORKSPACE).
+ */
+lshmoe_status lshmoe_expert_backward_weight(const void* grad_out, const void* x, const int32_t* expert_offsets,
+                                            int64_t rows, int32_t d_in, int32_t d_out, int32_t E, lshmoe_dtype dtype,
+                                            void* grad_w, void* grad_bias, void* workspace, size_t workspace_bytes,
+                                            void* stream);
+
+/*
+ * Microscaled 4-bit floating point (the MXFP4 format of the OCP Microscaling specification 1.0): 32 consecutive numbers
+ * of a row share a scale 2^s, stored as the byte s + 127; each number is a sign and a magnitude out of
+ * {0, 1/2, 1, 3/2, 2, 3, 4, 6}, four bits (sign, then the magnitude's number 0..7).
+ *     s = max(floor(log2 of the block's largest magnitude) - 2, -127);      number = the nearest multiple of 2^s that
+ * has a code, ties to the even code, magnitudes above 6 * 2^s to 6 * 2^s.  A block of zeros has scale byte 0.  A block that
+ * holds an infinity or a NaN gets scale byte 255 and codes 0 and reads as NaN throughout.
+ *
+ *   x      [rows, d]     in   dtype
+ *   codes  [rows, d/2]   out  bytes; byte i holds number 2i in its lower half and number 2i + 1 in its upper half
+ *   scales [rows, d/32]  out  bytes
+ *
+ * Errors: NULL pointer; rows, d <= 0 (SHAPE); unknown dtype, d not a multiple of 32, rows >= 2^30, more than about 64 GiB of
+ * rows, a pointer that is not 16-byte aligned (UNSUPPORTED); launch failure (HIP).
+ */
+lshmoe_status lshmoe_mx4_quantize(const void* x, int64_t rows, int32_t d, lshmoe_dtype dtype,
+                                  uint8_t* codes, uint8_t* scales, void* stream);
+
+/* The numbers that such rows stand for (exact in either dtype).  Arguments and errors as for lshmoe_mx4_quantize. */
+lshmoe_status lshmoe_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t d,
+                                    lshmoe_dtype dtype, void* out, void* stream);
+
+/*
+ * lshmoe_expert_forward on rows and weights in microscaled 4-bit floating point, for serving:
+ *     out[s, :] = act(W_e x[s, :] + b_e)     of the numbers that the codes and scales stand for,
+ * products exact, accumulated in binary32, rounded once to dtype.  Rows from expert_offsets[E] on are not read and not
+ * written.
+ *
+ *   x_codes [rows, d_in/2], x_scales [rows, d_in/32]                  in  as lshmoe_mx4_quantize writes them
+ *   w_codes [E, d_out, d_in/2], w_scales [E, d_out, d_in/32]          in  likewise, for E * d_out rows
+ *   bias [E, d_out]  in  dtype, or NULL
+ *   out [rows, d_out]  out  dtype
+ *   other arguments as for lshmoe_expert_forward.
+ *
+ * Errors: as for lshmoe_expert_forward; d_in not a multiple of 32 (UNSUPPORTED).
+ */
+lshmoe_status lshmoe_expert_forward_mx4(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes,
+                                        const uint8_t* w_scales, const void* bias, const int32_t* expert_offsets,
+                                        int64_t rows, int32_t d_in, int32_t d_out, int32_t E, lshmoe_dtype dtype,
+                                        lshmoe_activation act, void* out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -22,7 +22,11 @@ LSHMOE_ERR_HIP = 5
 LSHMOE_F32 = 0
 LSHMOE_BF16 = 1
 LSHMOE_FLAG_NO_RESIDUAL = 1
-ABI_VERSION = 6   # of include/lshmoe.h as this binding declares it
+LSHMOE_FLAG_GATE_FULL_SOFTMAX = 2
+LSHMOE_ACT_NONE = 0
+LSHMOE_ACT_RELU = 1
+LSHMOE_ACT_GELU = 2
+ABI_VERSION = 7   # of include/lshmoe.h as this binding declares it
 
 
 class LshmoeError(RuntimeError):
@@ -80,6 +84,24 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.lshmoe_decompress_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, ctypes.c_int, vp, vp, ctypes.c_size_t, vp]
     lib.lshmoe_compress_backward.restype = ctypes.c_int
     lib.lshmoe_compress_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, ctypes.c_int, u32, vp, vp]
+    lib.lshmoe_gate_topk.restype = ctypes.c_int
+    lib.lshmoe_gate_topk.argtypes = [vp, i64, i32, i32, u32, vp, vp, vp]
+    lib.lshmoe_gate_topk_backward.restype = ctypes.c_int
+    lib.lshmoe_gate_topk_backward.argtypes = [vp, vp, vp, vp, i64, i32, i32, u32, vp, vp]
+    lib.lshmoe_expert_forward.restype = ctypes.c_int
+    lib.lshmoe_expert_forward.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, ctypes.c_int, ctypes.c_int, vp, vp, vp]
+    lib.lshmoe_expert_backward_input.restype = ctypes.c_int
+    lib.lshmoe_expert_backward_input.argtypes = [vp, vp, vp, i64, i32, i32, i32, ctypes.c_int, ctypes.c_int, vp, vp, vp]
+    lib.lshmoe_expert_workspace_bytes.restype = ctypes.c_int
+    lib.lshmoe_expert_workspace_bytes.argtypes = [i64, i32, i32, i32, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+    lib.lshmoe_expert_backward_weight.restype = ctypes.c_int
+    lib.lshmoe_expert_backward_weight.argtypes = [vp, vp, vp, i64, i32, i32, i32, ctypes.c_int, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.lshmoe_mx4_quantize.restype = ctypes.c_int
+    lib.lshmoe_mx4_quantize.argtypes = [vp, i64, i32, ctypes.c_int, vp, vp, vp]
+    lib.lshmoe_mx4_dequantize.restype = ctypes.c_int
+    lib.lshmoe_mx4_dequantize.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, vp]
+    lib.lshmoe_expert_forward_mx4.restype = ctypes.c_int
+    lib.lshmoe_expert_forward_mx4.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, ctypes.c_int, ctypes.c_int, vp, vp]
     _lib = lib
     return lib
 
@@ -186,7 +208,7 @@ class CompressOutputs:
 def _aligned_ws(ws: torch.Tensor):
     base = ws.data_ptr()
     pad = (-base) % 256
-    return base + pad, ws.numel() - pad
+    return base + pad, max(ws.numel() - pad, 0)
 
 
 def lshmoe_compress(tokens: torch.Tensor, expert: torch.Tensor, bucket: torch.Tensor, E: int, L: int, r: int,
@@ -312,3 +334,132 @@ def lshmoe_compress_backward(grad_out, grad_centroids: torch.Tensor, grad_expert
     _check(load_library().lshmoe_compress_backward(
         _ptr(grad_out), _ptr(grad_centroids), _ptr(grad_expert_out), _ptr(seg_of, torch.int32),
         _ptr(seg_offsets, torch.int32), T, d, k, _dtype_code(grad_tokens), flags, _ptr(grad_tokens), _stream(stream)))
+
+
+def _one_device(*tensors) -> None:
+    """The launch goes to the current device: its tensors have to be there."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != device:
+            raise ValueError("a tensor is on %s, the current device is cuda:%d" % (t.device, device))
+
+
+def lshmoe_gate_topk(logits: torch.Tensor, expert: torch.Tensor, gate_weight: torch.Tensor, flags: int = 0,
+                     stream=None) -> None:
+    """logits [T, E] (float32) -> expert [T, k] (int32), largest first, and gate_weight [T, k] (float32)."""
+    T, E = logits.shape
+    k = expert.shape[1]
+    if expert.shape != (T, k) or gate_weight.shape != (T, k):
+        raise ValueError("expert and gate_weight must be [T, k]")
+    f32 = torch.float32
+    args = (_ptr(logits, f32), T, E, k, flags, _ptr(expert, torch.int32), _ptr(gate_weight, f32))
+    _one_device(logits, expert, gate_weight)
+    _check(load_library().lshmoe_gate_topk(*args, _stream(stream)))
+
+
+def lshmoe_gate_topk_backward(logits, expert: torch.Tensor, gate_weight: torch.Tensor, grad_gate_weight: torch.Tensor,
+                              grad_logits: torch.Tensor, flags: int = 0, stream=None) -> None:
+    """grad_gate_weight [T, k] -> grad_logits [T, E]; logits may be None without LSHMOE_FLAG_GATE_FULL_SOFTMAX."""
+    T, E = grad_logits.shape
+    k = expert.shape[1]
+    if expert.shape != (T, k) or gate_weight.shape != (T, k) or grad_gate_weight.shape != (T, k) \
+            or (logits is not None and logits.shape != (T, E)):
+        raise ValueError("expert, gate_weight and grad_gate_weight must be [T, k], logits and grad_logits [T, E]")
+    f32 = torch.float32
+    args = (_ptr(logits, f32), _ptr(expert, torch.int32), _ptr(gate_weight, f32), _ptr(grad_gate_weight, f32), T, E, k, flags,
+            _ptr(grad_logits, f32))
+    _one_device(logits, expert, gate_weight, grad_gate_weight, grad_logits)
+    _check(load_library().lshmoe_gate_topk_backward(*args, _stream(stream)))
+
+
+def lshmoe_expert_forward(x: torch.Tensor, w: torch.Tensor, bias, expert_offsets: torch.Tensor, out: torch.Tensor,
+                          act: int = LSHMOE_ACT_NONE, pre=None, stream=None) -> None:
+    """out [rows, d_out] = act(x [rows, d_in] @ w[e].T + bias[e]) for rows expert_offsets[e] .. expert_offsets[e + 1] - 1;
+    pre (optional) takes the values before the activation.  Rows from expert_offsets[E] on are left alone."""
+    rows, d_in = x.shape
+    E, d_out, d2 = w.shape
+    if d2 != d_in or out.shape != (rows, d_out) or expert_offsets.numel() != E + 1 \
+            or (bias is not None and bias.shape != (E, d_out)) or (pre is not None and pre.shape != (rows, d_out)):
+        raise ValueError("w must be [E, d_out, d_in], bias [E, d_out], expert_offsets [E + 1], out and pre [rows, d_out]")
+    dt = x.dtype
+    args = (_ptr(x), _ptr(w, dt), _ptr(bias, dt), _ptr(expert_offsets, torch.int32), rows, d_in, d_out, E, _dtype_code(x), act,
+            _ptr(pre, dt), _ptr(out, dt))
+    _one_device(x, w, bias, expert_offsets, pre, out)
+    _check(load_library().lshmoe_expert_forward(*args, _stream(stream)))
+
+
+def lshmoe_expert_backward_input(grad_out: torch.Tensor, w: torch.Tensor, expert_offsets: torch.Tensor,
+                                 grad_x: torch.Tensor, act: int = LSHMOE_ACT_NONE, pre=None, stream=None) -> None:
+    """grad_x [rows, d_in] = (grad_out [rows, d_out] @ w[e]) * act'(pre [rows, d_in])."""
+    rows, d_out = grad_out.shape
+    E, d2, d_in = w.shape
+    if d2 != d_out or grad_x.shape != (rows, d_in) or expert_offsets.numel() != E + 1 \
+            or (pre is not None and pre.shape != (rows, d_in)):
+        raise ValueError("w must be [E, d_out, d_in], expert_offsets [E + 1], grad_x and pre [rows, d_in]")
+    dt = grad_out.dtype
+    args = (_ptr(grad_out), _ptr(w, dt), _ptr(expert_offsets, torch.int32), rows, d_in, d_out, E, _dtype_code(grad_out), act,
+            _ptr(pre, dt), _ptr(grad_x, dt))
+    _one_device(grad_out, w, expert_offsets, pre, grad_x)
+    _check(load_library().lshmoe_expert_backward_input(*args, _stream(stream)))
+
+
+def lshmoe_expert_workspace_bytes(rows: int, d_in: int, d_out: int, E: int, dtype_code: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().lshmoe_expert_workspace_bytes(rows, d_in, d_out, E, dtype_code, ctypes.byref(out)))
+    return int(out.value)
+
+
+def lshmoe_expert_backward_weight(grad_out: torch.Tensor, x: torch.Tensor, expert_offsets: torch.Tensor,
+                                  grad_w: torch.Tensor, grad_bias, workspace: torch.Tensor, stream=None) -> None:
+    """grad_w[e] [d_out, d_in] = grad_out[rows of e].T @ x[rows of e] and (optional) grad_bias[e] = the sum of those rows."""
+    rows, d_out = grad_out.shape
+    E, d2, d_in = grad_w.shape
+    if d2 != d_out or x.shape != (rows, d_in) or expert_offsets.numel() != E + 1 \
+            or (grad_bias is not None and grad_bias.shape != (E, d_out)):
+        raise ValueError("x must be [rows, d_in], expert_offsets [E + 1], grad_w [E, d_out, d_in] and grad_bias [E, d_out]")
+    dt = grad_out.dtype
+    _ptr(workspace, torch.uint8)
+    ws_ptr, ws_bytes = _aligned_ws(workspace)
+    args = (_ptr(grad_out), _ptr(x, dt), _ptr(expert_offsets, torch.int32), rows, d_in, d_out, E, _dtype_code(grad_out),
+            _ptr(grad_w, dt), _ptr(grad_bias, dt), ws_ptr, ws_bytes)
+    _one_device(grad_out, x, expert_offsets, grad_w, grad_bias, workspace)
+    _check(load_library().lshmoe_expert_backward_weight(*args, _stream(stream)))
+
+
+def lshmoe_mx4_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """x [rows, d] -> codes [rows, d / 2] and scales [rows, d / 32] (uint8): blocks of 32 4-bit numbers with a scale."""
+    rows, d = x.shape
+    if codes.shape != (rows, d // 2) or scales.shape != (rows, d // 32):
+        raise ValueError("codes must be [rows, d / 2] and scales [rows, d / 32]")
+    args = (_ptr(x), rows, d, _dtype_code(x), _ptr(codes, torch.uint8), _ptr(scales, torch.uint8))
+    _one_device(x, codes, scales)
+    _check(load_library().lshmoe_mx4_quantize(*args, _stream(stream)))
+
+
+def lshmoe_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """codes [rows, d / 2] and scales [rows, d / 32] -> out [rows, d], the numbers that they stand for."""
+    rows, d = out.shape
+    if codes.shape != (rows, d // 2) or scales.shape != (rows, d // 32):
+        raise ValueError("codes must be [rows, d / 2] and scales [rows, d / 32]")
+    args = (_ptr(codes, torch.uint8), _ptr(scales, torch.uint8), rows, d, _dtype_code(out), _ptr(out))
+    _one_device(codes, scales, out)
+    _check(load_library().lshmoe_mx4_dequantize(*args, _stream(stream)))
+
+
+def lshmoe_expert_forward_mx4(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
+                              bias, expert_offsets: torch.Tensor, out: torch.Tensor, act: int = LSHMOE_ACT_NONE,
+                              stream=None) -> None:
+    """lshmoe_expert_forward on rows [rows, d_in] and weights [E, d_out, d_in] as lshmoe_mx4_quantize writes them."""
+    rows, half = x_codes.shape
+    E, d_out, half2 = w_codes.shape
+    d_in = 2 * half
+    if half2 != half or x_scales.shape != (rows, d_in // 32) or w_scales.shape != (E, d_out, d_in // 32) \
+            or out.shape != (rows, d_out) or expert_offsets.numel() != E + 1 \
+            or (bias is not None and bias.shape != (E, d_out)):
+        raise ValueError("x must be [rows, d_in], w [E, d_out, d_in] in blocks of 32, bias [E, d_out], expert_offsets [E + 1] "
+                         "and out [rows, d_out]")
+    u8 = torch.uint8
+    args = (_ptr(x_codes, u8), _ptr(x_scales, u8), _ptr(w_codes, u8), _ptr(w_scales, u8), _ptr(bias, out.dtype),
+            _ptr(expert_offsets, torch.int32), rows, d_in, d_out, E, _dtype_code(out), act, _ptr(out))
+    _one_device(x_codes, x_scales, w_codes, w_scales, bias, expert_offsets, out)
+    _check(load_library().lshmoe_expert_forward_mx4(*args, _stream(stream)))

@@ -20,7 +20,8 @@ LIB_PATH = os.path.join(LIB_DIR, "liblshmoe.so")
 PEAKS_LIB_PATH = os.path.join(LIB_DIR, "libpeaks.so")   # measured-peak probes of bench.py --peaks, not part of the path
 BUILD_DIR = os.path.join(ROOT, "_build")
 
-SOURCES = ["api.hip", "hash.hip", "group.hip", "centroid.hip", "restore.hip", "backward.hip"]
+SOURCES = ["api.hip", "hash.hip", "group.hip", "centroid.hip", "restore.hip", "backward.hip",
+           "api_experts.hip", "gate.hip", "experts.hip", "mx4.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

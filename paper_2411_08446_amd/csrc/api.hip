@@ -6,12 +6,14 @@
 
 #include <atomic>
 
-#include "../../include/lshmoe.h"
+#include "api.h"
 #include "kernels.h"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace lshmoe {
 
 lshmoe_status fail(lshmoe_status st, const char* fmt, ...) {
   va_list ap;
@@ -30,8 +32,24 @@ lshmoe_status hip_fail(const char* what, hipError_t e) {
   return fail(LSHMOE_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool dtype_ok(int dt) { return dt == LSHMOE_F32 || dt == LSHMOE_BF16; }
-size_t item_size(int dt) { return dt == LSHMOE_BF16 ? 2 : 4; }
+lshmoe_status check_row(int d, int dt) {
+  if (!dtype_ok(dt)) return fail(LSHMOE_ERR_UNSUPPORTED, "unknown dtype %d", dt);
+  if (((size_t)d * item_size(dt)) % 16 != 0)
+    return fail(LSHMOE_ERR_UNSUPPORTED, "row size d*sizeof(element) = %zu bytes is not a multiple of 16",
+                (size_t)d * item_size(dt));
+  return LSHMOE_OK;
+}
+
+}  // namespace lshmoe
+
+namespace {
+
+using lshmoe::check_row;
+using lshmoe::fail;
+using lshmoe::hip_fail;
+using lshmoe::item_size;
+using lshmoe::kMaxAssignments;
+using lshmoe::ok;
 
 // (2r)^L < 2^63 ?
 bool bucket_space_ok(int L, int r) {
@@ -41,16 +59,6 @@ bool bucket_space_ok(int L, int r) {
     if (nb >= ((unsigned __int128)1 << 63)) return false;
   }
   return true;
-}
-
-constexpr int64_t kMaxAssignments = (int64_t)1 << 30;
-
-lshmoe_status check_row(int d, int dt) {
-  if (!dtype_ok(dt)) return fail(LSHMOE_ERR_UNSUPPORTED, "unknown dtype %d", dt);
-  if (((size_t)d * item_size(dt)) % 16 != 0)
-    return fail(LSHMOE_ERR_UNSUPPORTED, "row size d*sizeof(element) = %zu bytes is not a multiple of 16",
-                (size_t)d * item_size(dt));
-  return LSHMOE_OK;
 }
 
 lshmoe_status check_hash_params(int L, int r) {
@@ -160,7 +168,7 @@ const char* lshmoe_status_string(int status) {
 
 const char* lshmoe_last_error(void) { return g_err; }
 
-int lshmoe_abi_version(void) { return 6; }
+int lshmoe_abi_version(void) { return 7; }
 
 lshmoe_status lshmoe_workspace_bytes(int64_t T, int32_t d, int32_t k, int32_t E, int32_t L, int32_t r,
                                      lshmoe_dtype dtype, size_t* out_bytes) {

@@ -96,4 +96,30 @@ hipError_t launch_combine_backward(const void* tokens, const void* centroids, co
                                    const void* grad_out, float* grad_w, void* grad_rows, int64_t T, int k, int d, bool bf16,
                                    uint32_t flags, hipStream_t stream);
 
+// ---- router ---------------------------------------------------------------
+constexpr int kMaxGateExperts = 1024, kMaxGateChoices = 64;
+hipError_t launch_gate_topk(const float* logits, int64_t T, int E, int k, bool full, int32_t* expert, float* weight,
+                            hipStream_t stream);
+hipError_t launch_gate_topk_backward(const float* logits, const int32_t* expert, const float* weight,
+                                     const float* grad_weight, int64_t T, int E, int k, bool full, float* grad_logits,
+                                     hipStream_t stream);
+
+// ---- experts' products on rows grouped by expert ---------------------------
+hipError_t launch_expert_forward(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows,
+                                 int d_in, int d_out, int E, bool bf16, int act, void* pre, void* out, hipStream_t stream);
+hipError_t launch_expert_input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in,
+                                    int d_out, int E, bool bf16, int act, const void* pre, void* grad_x, hipStream_t stream);
+size_t expert_workspace_bytes(int64_t rows, int d_in, int d_out, int E, bool bf16);
+hipError_t launch_expert_weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in,
+                                     int d_out, int E, bool bf16, void* grad_w, void* grad_bias, char* workspace,
+                                     hipStream_t stream);
+
+// ---- microscaled 4-bit rows -------------------------------------------------
+hipError_t launch_mx4_quantize(const void* x, int64_t rows, int d, bool bf16, void* codes, uint8_t* scales, hipStream_t stream);
+hipError_t launch_mx4_dequantize(const void* codes, const uint8_t* scales, int64_t rows, int d, bool bf16, void* out,
+                                 hipStream_t stream);
+hipError_t launch_expert_forward_mx4(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
+                                     const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
+                                     bool bf16, int act, void* out, hipStream_t stream);
+
 }  // namespace lshmoe

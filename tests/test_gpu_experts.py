@@ -1,0 +1,495 @@
+"""Router, experts' products and 4-bit rows on the GPU against the binary64 oracle.
+
+Bounds.  A product of K terms summed in binary32 in any order is off by at most (K + 4) 2^-24 times the sum of the terms'
+magnitudes (bf16 and 4-bit products are exact); its rounding to the storage type adds half a step, eps / 2 of the value.  The
+GELU's value adds |v| 2^-21 (the distribution function to 8 units of 2^-24 and two roundings) and passes an error of its
+argument on at most 1.13-fold; the slope is good to 2^-20.  Bounds hold element by element."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2411_08446_amd as lsh
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+ACT = {"none": lsh.LSHMOE_ACT_NONE, "relu": lsh.LSHMOE_ACT_RELU, "gelu": lsh.LSHMOE_ACT_GELU}
+
+
+def _code(dtype):
+    return lsh.LSHMOE_F32 if dtype == "f32" else lsh.LSHMOE_BF16
+
+
+def _wide(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _assert_within(got, want, bound, what):
+    got, bound = _wide(got) if torch.is_tensor(got) else got, bound + 1e-300
+    assert not np.isnan(got).any(), "%s: NaN at %s" % (what, np.argwhere(np.isnan(got))[:4].tolist())
+    excess = np.abs(got - want) / bound
+    assert excess.max(initial=0.0) <= 1.0, "%s: %.3g of the bound at %s" % (what, excess.max(), np.unravel_index(excess.argmax(), excess.shape))
+
+
+def _rounded(size, K, dtype, want, lipschitz=1.0, extra=0.0):
+    before = lipschitz * (K + 4) * 2.0 ** -24 * size + extra
+    return before + HALF_STEP[dtype] * (np.abs(want) + before)
+
+
+def _offsets(counts):
+    return [0] + np.cumsum(counts).tolist()
+
+
+def _workspace(rows, d_in, d_out, E, dtype):
+    n = lsh.lshmoe_expert_workspace_bytes(rows, d_in, d_out, E, _code(dtype))
+    return torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+
+
+# ---- router ------------------------------------------------------------------
+
+def _gate_bounds(logits, ids, weight, full):
+    """exp of a difference l - m: the difference is rounded (2^-24 of it), the function good to 2 units; a sum of at most E such
+    terms, a division."""
+    with np.errstate(invalid="ignore"):
+        span = np.where(np.isfinite(logits), logits, np.nan)
+    span = np.nan_to_num(np.nanmax(span, axis=1, initial=0) - np.nanmin(span, axis=1, initial=0))[:, None]
+    return (2 * span + logits.shape[1] + 12) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 2, 2), (37, 16, 2), (5, 3, 3), (257, 6, 2), (64, 8, 8), (100, 17, 4), (33, 33, 5),
+                                   (130, 60, 6), (64, 64, 1), (63, 64, 64), (40, 128, 8), (31, 129, 2), (20, 256, 6),
+                                   (9, 333, 7), (7, 512, 3), (6, 1000, 64), (3, 1024, 2)])
+@pytest.mark.parametrize("full", [False, True])
+def test_gate(T, E, k, full):
+    rng = np.random.default_rng(T * 1000 + E)
+    logits = rng.standard_normal((T, E)).astype(np.float32) * 2
+    logits[T // 3:T // 2 + 1] = np.round(logits[T // 3:T // 2 + 1])          # many ties
+    if T > 4:
+        logits[1, rng.random(E) < 0.5] = -np.inf
+        logits[2] = -np.inf
+        logits[3] = 0.0
+        logits[4, : E // 2] = -0.0
+        logits[4, E // 2:] = 0.0
+    flags = lsh.LSHMOE_FLAG_GATE_FULL_SOFTMAX if full else 0
+    lt = torch.from_numpy(logits).cuda()
+    ids = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
+    w = torch.full((T, k), float("nan"), device="cuda")
+    lsh.lshmoe_gate_topk(lt, ids, w, flags=flags)
+    ref_ids, ref_w = oracle.gate_topk_ref(logits.astype(np.float64), k, full)
+    assert np.array_equal(ids.cpu().numpy(), ref_ids)
+    rel = _gate_bounds(logits, ref_ids, ref_w, full)
+    _assert_within(w, ref_w, rel * ref_w, "weights")
+
+    g = rng.standard_normal((T, k)).astype(np.float32)
+    out = torch.full((T, E), float("nan"), device="cuda")
+    lsh.lshmoe_gate_topk_backward(lt if full else None, ids, w, torch.from_numpy(g).cuda(), out, flags=flags)
+    ref = oracle.gate_topk_backward_ref(logits.astype(np.float64), ref_ids, g.astype(np.float64), full)
+    p = np.zeros((T, E))
+    if full:
+        top = logits.max(axis=1, keepdims=True).astype(np.float64)
+        with np.errstate(invalid="ignore"):
+            p = np.nan_to_num(np.exp(logits - top))
+        p = p / np.maximum(p.sum(axis=1, keepdims=True), 1e-300)
+    else:
+        np.put_along_axis(p, ref_ids.astype(np.int64), ref_w, axis=1)
+    # p (g - h): p and the weights in h are off by rel, h is a sum of k products, the difference rounds once
+    size = np.abs(g).max(axis=1, keepdims=True) * 2
+    _assert_within(out, ref, p * size * (2 * rel + (k + 4) * 2.0 ** -24), "logit gradient")
+
+
+def test_gate_of_infinities_and_nan():
+    nan, inf = float("nan"), float("inf")
+    rows = [[0.0, nan, 1.0, nan, 2.0], [1.0, inf, 0.0, -inf, inf], [-inf, -inf, -inf, 3.0, -inf], [nan] * 5]
+    lt = torch.tensor(rows, device="cuda")
+    ids = torch.empty(4, 3, dtype=torch.int32, device="cuda")
+    w = torch.empty(4, 3, device="cuda")
+    lsh.lshmoe_gate_topk(lt, ids, w)
+    assert ids.tolist() == [[1, 3, 4], [1, 4, 0], [3, 0, 1], [0, 1, 2]]
+    assert torch.isnan(w[0]).all() and torch.isnan(w[1]).all() and torch.isnan(w[3]).all()
+    assert w[2].tolist() == [1.0, 0.0, 0.0]
+
+
+def test_gate_backward_adds_up_a_repeated_expert_and_bounds_ids():
+    ids = torch.tensor([[1, 1], [7, -1]], dtype=torch.int32, device="cuda")
+    w = torch.tensor([[0.5, 0.25], [0.5, 0.5]], device="cuda")
+    g = torch.tensor([[1.0, 2.0], [1.0, 3.0]], device="cuda")
+    out = torch.full((2, 4), float("nan"), device="cuda")
+    lsh.lshmoe_gate_topk_backward(None, ids, w, g, out)
+    assert out[0].tolist() == [0.0, 0.5 * (1 - 1.0) + 0.25 * (2 - 1.0), 0.0, 0.0]
+    assert out[1].tolist() == [0.0, 0.0, 0.0, 0.5 * (1 - 2.0) + 0.5 * (3 - 2.0)]
+
+
+# ---- products ------------------------------------------------------------------
+
+# rows of each expert, rows behind the last one, d_in, d_out
+SHAPES = [
+    ([1], 0, 8, 8),
+    ([0, 1, 0], 3, 16, 24),
+    ([0, 0], 5, 64, 64),
+    ([3, 0, 17, 1], 2, 72, 40),
+    ([5, 70, 1, 0, 33], 9, 136, 200),
+    ([64, 128, 192], 0, 64, 128),
+    ([130, 1, 255, 257], 1, 264, 136),
+    ([2] * 70, 6, 40, 72),
+    ([600, 0, 20], 11, 128, 512),
+    ([16] * 4, 0, 1000, 1504),
+    ([1300], 4, 512, 256),
+    ([37, 290, 511], 3, 1024, 784),
+]
+
+
+def _inputs(counts, spare, d_in, d_out, dtype, seed, poison=float("nan")):
+    gen = torch.Generator().manual_seed(seed)
+    rows, E = sum(counts) + spare, len(counts)
+    filled = sum(counts)
+
+    def make(*shape):
+        return torch.randn(*shape, generator=gen).to(DT[dtype])
+    t = {"x": make(rows, d_in), "g": make(rows, d_out), "pre": make(rows, d_in), "w": make(E, d_out, d_in), "b": make(E, d_out)}
+    for n in ("x", "g", "pre"):
+        t[n][filled:] = poison                        # rows behind the last expert's are not read
+    dev = {n: v.cuda() for n, v in t.items()}
+    dev["off"] = torch.tensor(_offsets(counts), dtype=torch.int32, device="cuda")
+    ref = {n: v.double().numpy() for n, v in t.items()}
+    for n in ("x", "g", "pre"):
+        ref[n][filled:] = 0.0
+    return rows, E, filled, dev, ref
+
+
+def _blank(*shape, dtype):
+    return torch.full(shape, 7.0, dtype=DT[dtype], device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act,bias,keep", [("none", False, False), ("relu", True, True), ("gelu", True, True), ("gelu", False, False)])
+@pytest.mark.parametrize("counts,spare,d_in,d_out", SHAPES)
+def test_expert_forward(counts, spare, d_in, d_out, act, bias, keep, dtype):
+    rows, E, filled, dev, ref = _inputs(counts, spare, d_in, d_out, dtype, 1 + d_in)
+    out, pre = _blank(rows, d_out, dtype=dtype), _blank(rows, d_out, dtype=dtype) if keep else None
+    lsh.lshmoe_expert_forward(dev["x"], dev["w"], dev["b"] if bias else None, dev["off"], out, act=ACT[act], pre=pre)
+    off = _offsets(counts)
+    want_pre, want, size = oracle.expert_forward_ref(ref["x"], ref["w"], ref["b"] if bias else None, off, act)
+    extra = np.abs(want_pre) * 2.0 ** -21 if act == "gelu" else 0.0
+    lipschitz = 1.13 if act == "gelu" else 1.0
+    bound = _rounded(size, d_in, dtype, want, lipschitz, extra)
+    _assert_within(out[:filled], want[:filled], bound[:filled], "out")
+    assert (out[filled:] == 7.0).all(), "rows behind the last expert's are left alone"
+    if keep:
+        _assert_within(pre[:filled], want_pre[:filled], _rounded(size, d_in, dtype, want_pre)[:filled], "pre")
+        assert (pre[filled:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("counts,spare,d_in,d_out", SHAPES)
+def test_expert_backward_input(counts, spare, d_in, d_out, act, dtype):
+    rows, E, filled, dev, ref = _inputs(counts, spare, d_in, d_out, dtype, 2 + d_in)
+    gx = _blank(rows, d_in, dtype=dtype)
+    lsh.lshmoe_expert_backward_input(dev["g"], dev["w"], dev["off"], gx, act=ACT[act], pre=None if act == "none" else dev["pre"])
+    want, plain, slope, size = oracle.expert_backward_input_ref(ref["g"], ref["w"], _offsets(counts), act, ref["pre"])
+    extra = (np.abs(plain) + size * (d_out + 4) * 2.0 ** -24) * (2.0 ** -20 + 2.0 ** -24 if act == "gelu" else 0.0)
+    bound = _rounded(size * np.abs(slope), d_out, dtype, want, 1.0, extra)
+    _assert_within(gx[:filled], want[:filled], bound[:filled], "grad_x")
+    assert (gx[filled:] == 7.0).all(), "rows behind the last expert's are left alone"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("counts,spare,d_in,d_out", SHAPES)
+def test_expert_backward_weight(counts, spare, d_in, d_out, bias, dtype):
+    rows, E, filled, dev, ref = _inputs(counts, spare, d_in, d_out, dtype, 3 + d_in)
+    gw, gb = _blank(E, d_out, d_in, dtype=dtype), _blank(E, d_out, dtype=dtype) if bias else None
+    lsh.lshmoe_expert_backward_weight(dev["g"], dev["x"], dev["off"], gw, gb, _workspace(rows, d_in, d_out, E, dtype))
+    want_w, want_b, size_w, size_b = oracle.expert_backward_weight_ref(ref["g"], ref["x"], _offsets(counts), E)
+    K = max(counts)
+    _assert_within(gw, want_w, _rounded(size_w, K, dtype, want_w), "grad_w")
+    if bias:
+        _assert_within(gb, want_b, _rounded(size_b, K, dtype, want_b), "grad_bias")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_is_not_finite_stays_with_its_rows(dtype):
+    """An expert whose rows hold infinities and NaN changes nothing of its neighbours', at sizes that are no whole tiles."""
+    counts, d_in, d_out = [37, 50, 41], 72, 88
+    rows, E, filled, dev, ref = _inputs(counts, 7, d_in, d_out, dtype, 9)
+    clean = [t.clone() for t in (dev["x"], dev["g"])]
+    ws = _workspace(rows, d_in, d_out, E, dtype)
+    results = []
+    for dirty in (False, True):
+        x, g, w = clean[0].clone(), clean[1].clone(), dev["w"].clone()
+        if dirty:
+            x[37:87] = float("inf")
+            g[37:87] = float("nan")
+            w[1] = float("nan")
+        out, gx = _blank(rows, d_out, dtype=dtype), _blank(rows, d_in, dtype=dtype)
+        gw, gb = _blank(E, d_out, d_in, dtype=dtype), _blank(E, d_out, dtype=dtype)
+        lsh.lshmoe_expert_forward(x, w, dev["b"], dev["off"], out)
+        lsh.lshmoe_expert_backward_input(g, w, dev["off"], gx)
+        lsh.lshmoe_expert_backward_weight(g, x, dev["off"], gw, gb, ws)
+        results.append((out, gx, gw, gb))
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[37:87] = False
+    a, b = results
+    assert torch.equal(a[0][keep], b[0][keep]) and torch.equal(a[1][keep], b[1][keep])
+    for e in (0, 2):
+        assert torch.equal(a[2][e], b[2][e]) and torch.equal(a[3][e], b[3][e])
+    assert torch.isnan(b[0][37:87].float()).all() and torch.isnan(b[1][37:87].float()).all()
+    assert torch.isnan(b[2][1].float()).all() and torch.isnan(b[3][1].float()).all()
+
+
+def test_offsets_out_of_range_stay_in_bounds():
+    """Offsets beyond the rows count as the nearest row; nothing outside the buffers is touched."""
+    rows, d_in, d_out, E = 40, 64, 64, 3
+    gen = torch.Generator().manual_seed(5)
+    x, w = torch.randn(rows, d_in, generator=gen).cuda(), torch.randn(E, d_out, d_in, generator=gen).cuda()
+    out = torch.full((rows, d_out), 7.0, device="cuda")
+    lsh.lshmoe_expert_forward(x, w, None, torch.tensor([-5, 10, 30, 1000], dtype=torch.int32, device="cuda"), out)
+    same = torch.full((rows, d_out), 7.0, device="cuda")
+    lsh.lshmoe_expert_forward(x, w, None, torch.tensor([0, 10, 30, 40], dtype=torch.int32, device="cuda"), same)
+    assert torch.equal(out, same)
+
+
+# ---- 4-bit rows ----------------------------------------------------------------
+
+def _every_bf16():
+    """Every bf16 number beside a partner that sets the block's scale, in blocks of 32."""
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    return bits.view(-1, 32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,d", [(1, 32), (3, 64), (37, 768), (130, 160), (5, 4096), (1029, 96)])
+def test_quantize(rows, d, dtype):
+    gen = torch.Generator().manual_seed(rows + d)
+    x = torch.randn(rows, d, generator=gen) * torch.exp(4 * torch.randn(rows, 1, generator=gen))
+    x[:, ::7] = torch.round(x[:, ::7] * 4) / 4                              # ties
+    x[rows // 2, :32] = 0.0
+    x = x.to(DT[dtype])
+    codes = torch.full((rows, d // 2), 0xEE, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, d // 32), 0xEE, dtype=torch.uint8, device="cuda")
+    back = torch.full((rows, d), float("nan"), dtype=DT[dtype], device="cuda")
+    lsh.lshmoe_mx4_quantize(x.cuda(), codes, scales)
+    lsh.lshmoe_mx4_dequantize(codes, scales, back)
+    ref_codes, ref_scales = oracle.mx4_quantize_ref(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), ref_scales)
+    assert np.array_equal(codes.cpu().numpy(), ref_codes)
+    assert np.array_equal(_wide(back), oracle.mx4_values_ref(ref_codes, ref_scales))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize_every_number(dtype):
+    """All bf16 patterns, subnormals, infinities and NaN among them; blocks of neighbours, and each under a larger top."""
+    near = _every_bf16()
+    tops = near[torch.randperm(near.shape[0], generator=torch.Generator().manual_seed(1))].clone()
+    tops[:, 1:] = near[:, 1:]
+    x = torch.cat([near, tops]).contiguous().to(DT[dtype])
+    rows = x.shape[0]
+    codes = torch.empty(rows, 16, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(rows, 1, dtype=torch.uint8, device="cuda")
+    back = torch.empty(rows, 32, dtype=DT[dtype], device="cuda")
+    lsh.lshmoe_mx4_quantize(x.cuda(), codes, scales)
+    lsh.lshmoe_mx4_dequantize(codes, scales, back)
+    ref_codes, ref_scales = oracle.mx4_quantize_ref(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), ref_scales) and np.array_equal(codes.cpu().numpy(), ref_codes)
+    assert np.array_equal(_wide(back), oracle.mx4_values_ref(ref_codes, ref_scales), equal_nan=True)
+
+
+def test_read_back_of_every_code_and_scale():
+    codes = torch.arange(256, dtype=torch.uint8).repeat(16).view(256, 16).cuda()
+    scales = torch.arange(256, dtype=torch.uint8).view(256, 1).cuda()
+    for dtype in DT:
+        out = torch.zeros(256, 32, dtype=DT[dtype], device="cuda")
+        lsh.lshmoe_mx4_dequantize(codes, scales, out)
+        want = torch.from_numpy(oracle.mx4_values_ref(codes.cpu().numpy(), scales.cpu().numpy())).to(DT[dtype]).double().numpy()
+        assert np.array_equal(_wide(out), want, equal_nan=True)
+
+
+SHAPES_MX4 = [([1], 0, 32, 8), ([0, 1, 0], 3, 64, 24), ([3, 0, 17, 1], 2, 96, 40), ([5, 70, 1, 0, 33], 9, 160, 200),
+              ([64, 128, 192], 0, 128, 128), ([130, 1, 255, 257], 1, 288, 136), ([2] * 70, 6, 32, 72), ([600, 0, 20], 11, 256, 512),
+              ([16] * 4, 0, 992, 1504), ([1300], 4, 512, 256), ([37, 290, 511], 3, 1024, 784), ([0, 0], 4, 64, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act,bias", [("none", False), ("relu", True), ("gelu", True)])
+@pytest.mark.parametrize("counts,spare,d_in,d_out", SHAPES_MX4)
+def test_expert_forward_mx4(counts, spare, d_in, d_out, act, bias, dtype):
+    rows, E, filled, dev, ref = _inputs(counts, spare, d_in, d_out, dtype, 4 + d_in)
+    u8 = dict(dtype=torch.uint8, device="cuda")
+    xc, xs = torch.empty(rows, d_in // 2, **u8), torch.empty(rows, d_in // 32, **u8)
+    wc, wsc = torch.empty(E, d_out, d_in // 2, **u8), torch.empty(E, d_out, d_in // 32, **u8)
+    lsh.lshmoe_mx4_quantize(dev["x"], xc, xs)
+    lsh.lshmoe_mx4_quantize(dev["w"].view(E * d_out, d_in), wc.view(E * d_out, -1), wsc.view(E * d_out, -1))
+    out = _blank(rows, d_out, dtype=dtype)
+    lsh.lshmoe_expert_forward_mx4(xc, xs, wc, wsc, dev["b"] if bias else None, dev["off"], out, act=ACT[act])
+    x4 = np.nan_to_num(oracle.mx4_values_ref(xc.cpu().numpy(), xs.cpu().numpy()))
+    w4 = oracle.mx4_values_ref(wc.cpu().numpy(), wsc.cpu().numpy())
+    want_pre, want, size = oracle.expert_forward_ref(x4, w4, ref["b"] if bias else None, _offsets(counts), act)
+    extra = np.abs(want_pre) * 2.0 ** -21 if act == "gelu" else 0.0
+    bound = _rounded(size, d_in, dtype, want, 1.13 if act == "gelu" else 1.0, extra)
+    _assert_within(out[:filled], want[:filled], bound[:filled], "out")
+    assert (out[filled:] == 7.0).all(), "rows behind the last expert's are left alone"
+
+
+def test_mx4_block_of_nan_reaches_its_row_only():
+    d_in, d_out = 160, 72
+    gen = torch.Generator().manual_seed(8)
+    x = torch.randn(40, d_in, generator=gen)
+    x[7, 100] = float("inf")
+    w = torch.randn(1, d_out, d_in, generator=gen)
+    u8 = dict(dtype=torch.uint8, device="cuda")
+    xc, xs, wc, wsc = (torch.empty(40, d_in // 2, **u8), torch.empty(40, d_in // 32, **u8),
+                       torch.empty(1, d_out, d_in // 2, **u8), torch.empty(1, d_out, d_in // 32, **u8))
+    lsh.lshmoe_mx4_quantize(x.cuda(), xc, xs)
+    lsh.lshmoe_mx4_quantize(w[0].cuda(), wc[0], wsc[0])
+    out = torch.zeros(40, d_out, device="cuda")
+    lsh.lshmoe_expert_forward_mx4(xc, xs, wc, wsc, None, torch.tensor([0, 40], dtype=torch.int32, device="cuda"), out)
+    bad = torch.isnan(out).all(dim=1)
+    assert bad.nonzero().flatten().tolist() == [7] and torch.isfinite(out[~bad]).all()
+
+
+# ---- together ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_layer_forward_and_backward(dtype):
+    """Hash and gate, choice, compression, a two-layer expert, restoration, and the way back, as a training step calls them;
+    every operator against the oracle on what the one before it left."""
+    T, d, h, k, E, L, r = 300, 256, 320, 2, 6, 2, 8
+    dt, code, N = DT[dtype], _code(dtype), 300 * 2
+    gen = torch.Generator().manual_seed(11)
+    centers = torch.randn(20, d, generator=gen)
+    x = (centers[torch.randint(20, (T,), generator=gen)] + 0.05 * torch.randn(T, d, generator=gen)).to(dt).cuda()
+    rot, gate_w = torch.randn(L, r, d, generator=gen).to(dt).cuda(), (torch.randn(E, d, generator=gen) / 16).to(dt).cuda()
+    w1, w2 = (torch.randn(E, h, d, generator=gen) / 16).to(dt).cuda(), (torch.randn(E, d, h, generator=gen) / 18).to(dt).cuda()
+    b1, b2 = torch.randn(E, h, generator=gen).to(dt).cuda(), torch.randn(E, d, generator=gen).to(dt).cuda()
+    bucket = torch.empty(T, dtype=torch.int64, device="cuda")
+    logits = torch.empty(T, E, device="cuda")
+    expert = torch.empty(T, k, dtype=torch.int32, device="cuda")
+    weight = torch.empty(T, k, device="cuda")
+    o = lsh.CompressOutputs.allocate(T, d, k, E, L, r, dt)
+    ws = _workspace(N, d, h, E, dtype)
+    ws2 = _workspace(N, h, d, E, dtype)
+    back_ws = torch.empty(lsh.lshmoe_backward_workspace_bytes(T, d, k, code) + 256, dtype=torch.uint8, device="cuda")
+
+    def buf(*shape, t=dt):
+        return torch.full(shape, 7.0, dtype=t, device="cuda")
+    pre, hid, eo, y = buf(N, h), buf(N, h), buf(N, d), buf(T, d)
+    gy = torch.randn(T, d, generator=gen).to(dt).cuda()
+    gwt, grows, geo, gpre, gc, gx, glog = (buf(T, k, t=torch.float32), buf(T, k, d), buf(N, d), buf(N, h), buf(N, d), buf(T, d),
+                                           buf(T, E, t=torch.float32))
+    gw1, gb1, gw2, gb2 = buf(E, h, d), buf(E, h), buf(E, d, h), buf(E, d)
+
+    def step():
+        lsh.lshmoe_hash_gate(x, rot, gate_w, bucket, logits)
+        lsh.lshmoe_gate_topk(logits, expert, weight)
+        lsh.lshmoe_compress(x, expert, bucket, E, L, r, o)
+        lsh.lshmoe_expert_forward(o.centroids, w1, b1, o.expert_offsets, hid, act=lsh.LSHMOE_ACT_GELU, pre=pre)
+        lsh.lshmoe_expert_forward(hid, w2, b2, o.expert_offsets, eo)
+        lsh.lshmoe_decompress_combine(x, o.centroids, eo, o.seg_of, o.seg_offsets, weight, y)
+        lsh.lshmoe_decompress_combine_backward(x, o.centroids, eo, o.seg_of, o.seg_offsets, weight, gy, gwt, grows)
+        lsh.lshmoe_gate_topk_backward(logits, expert, weight, gwt, glog)
+        lsh.lshmoe_decompress_backward(grows, o.perm, o.seg_offsets, o.seg_of, o.num_segments, geo, back_ws)
+        lsh.lshmoe_expert_backward_weight(geo, hid, o.expert_offsets, gw2, gb2, ws2)
+        lsh.lshmoe_expert_backward_input(geo, w2, o.expert_offsets, gpre, act=lsh.LSHMOE_ACT_GELU, pre=pre)
+        lsh.lshmoe_expert_backward_weight(gpre, o.centroids, o.expert_offsets, gw1, gb1, ws)
+        lsh.lshmoe_expert_backward_input(gpre, w1, o.expert_offsets, gc)
+        lsh.lshmoe_compress_backward(grows, gc, geo, o.seg_of, o.seg_offsets, k, gx)
+
+    step()
+    torch.cuda.synchronize()
+    S, off = int(o.num_segments.item()), o.expert_offsets.tolist()
+    assert 0 < S < N and off[-1] == S
+    ids, wref = oracle.gate_topk_ref(_wide(logits), k, False)
+    assert np.array_equal(expert.cpu().numpy(), ids)
+    _assert_within(weight, wref, _gate_bounds(_wide(logits), ids, wref, False) * wref, "weights")
+    wide = {n: _wide(t) for n, t in dict(c=o.centroids[:S], hid=hid[:S], w1=w1, w2=w2, b1=b1, b2=b2, pre=pre[:S], geo=geo[:S],
+                                         gpre=gpre[:S]).items()}
+    p_ref, h_ref, size = oracle.expert_forward_ref(wide["c"], wide["w1"], wide["b1"], off, "gelu")
+    _assert_within(pre[:S], p_ref, _rounded(size, d, dtype, p_ref), "pre")
+    _assert_within(hid[:S], h_ref, _rounded(size, d, dtype, h_ref, 1.13, np.abs(p_ref) * 2.0 ** -21), "hidden")
+    e_ref, _, size = oracle.expert_forward_ref(wide["hid"], wide["w2"], wide["b2"], off, "none")
+    _assert_within(eo[:S], e_ref, _rounded(size, h, dtype, e_ref), "expert output")
+    for t in (pre, hid, eo, gpre, gc):
+        assert (t[S:] == 7.0).all()
+    want, plain, slope, size = oracle.expert_backward_input_ref(wide["geo"], wide["w2"], off, "gelu", wide["pre"])
+    extra = (np.abs(plain) + size * (d + 4) * 2.0 ** -24) * (2.0 ** -20 + 2.0 ** -24)
+    _assert_within(gpre[:S], want, _rounded(size * np.abs(slope), d, dtype, want, 1.0, extra), "gradient before the activation")
+    want, _, _, size = oracle.expert_backward_input_ref(wide["gpre"], wide["w1"], off, "none", None)
+    _assert_within(gc[:S], want, _rounded(size, h, dtype, want), "centroid gradient")
+    for g, v, gw, gb in (("geo", "hid", gw2, gb2), ("gpre", "c", gw1, gb1)):
+        ww, wb, sw, sb = oracle.expert_backward_weight_ref(wide[g], wide[v], off, E)
+        _assert_within(gw, ww, _rounded(sw, S, dtype, ww), "weight gradient")
+        _assert_within(gb, wb, _rounded(sb, S, dtype, wb), "bias gradient")
+    ref = oracle.gate_topk_backward_ref(_wide(logits), ids, _wide(gwt), False)
+    p = np.zeros((T, E))
+    np.put_along_axis(p, ids.astype(np.int64), wref, axis=1)
+    rel = _gate_bounds(_wide(logits), ids, wref, False)
+    _assert_within(glog, ref, p * 2 * np.abs(_wide(gwt)).max(axis=1, keepdims=True) * (2 * rel + (k + 4) * 2.0 ** -24), "logit gradient")
+
+    # the whole step in a graph, replayed on new tokens with eager work between, against the eager step
+    outs = (y, gx, gw1, gb1, gw2, gb2, glog, weight)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        x.copy_((centers[torch.randint(20, (T,), generator=gen)] + 0.05 * torch.randn(T, d, generator=gen)).to(dt))
+        for t in outs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, outs):
+            assert torch.equal(a, b), "a replay gives what the eager step gives, bit for bit"
+
+
+def test_two_streams_at_once():
+    """Two weight gradients that overlap, each with its own workspace, give what they give alone."""
+    counts, d_in, d_out = [900, 10, 300], 264, 136
+    rows, E, filled, dev, _ = _inputs(counts, 0, d_in, d_out, "bf16", 21)
+    ws = [_workspace(rows, d_in, d_out, E, "bf16") for _ in range(2)]
+    alone, alone_b = _blank(E, d_out, d_in, dtype="bf16"), _blank(E, d_out, dtype="bf16")
+    lsh.lshmoe_expert_backward_weight(dev["g"], dev["x"], dev["off"], alone, alone_b, ws[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [(_blank(E, d_out, d_in, dtype="bf16"), _blank(E, d_out, dtype="bf16")) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, w, (gw, gb) in zip(streams, ws, outs):
+            lsh.lshmoe_expert_backward_weight(dev["g"], dev["x"], dev["off"], gw, gb, w, stream=s)
+    torch.cuda.synchronize()
+    for gw, gb in outs:
+        assert torch.equal(gw, alone) and torch.equal(gb, alone_b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_shapes_against_the_same_call_on_parts(dtype):
+    """Many rows and wide weights: parts of the outputs against binary64 products of the same rows."""
+    counts, d_in, d_out = [3000, 0, 1, 4097, 200, 900], 1096, 2056
+    rows, E, filled, dev, _ = _inputs(counts, 13, d_in, d_out, dtype, 31)
+    out, gx = _blank(rows, d_out, dtype=dtype), _blank(rows, d_in, dtype=dtype)
+    gw, gb = _blank(E, d_out, d_in, dtype=dtype), _blank(E, d_out, dtype=dtype)
+    lsh.lshmoe_expert_forward(dev["x"], dev["w"], dev["b"], dev["off"], out)
+    lsh.lshmoe_expert_backward_input(dev["g"], dev["w"], dev["off"], gx)
+    lsh.lshmoe_expert_backward_weight(dev["g"], dev["x"], dev["off"], gw, gb, _workspace(rows, d_in, d_out, E, dtype))
+    off = _offsets(counts)
+    assert (out[filled:] == 7.0).all() and (gx[filled:] == 7.0).all()
+    for e in range(E):
+        lo, hi = off[e], off[e + 1]
+        x, g, w = dev["x"][lo:hi].double(), dev["g"][lo:hi].double(), dev["w"][e].double()
+        for got, a, b, bias, K in ((out[lo:hi], x, w.t().contiguous(), dev["b"][e].double(), d_in), (gx[lo:hi], g, w, None, d_out),
+                                   (gw[e], g.t().contiguous(), x, None, hi - lo)):
+            want, size = torch.mm(a, b), torch.mm(a.abs(), b.abs())
+            if bias is not None:
+                want, size = want + bias, size + bias.abs()
+            _assert_within(got, want.cpu().numpy(), _rounded(size.cpu().numpy(), K, dtype, want.cpu().numpy()), "expert %d" % e)
+        want, size = g.sum(dim=0).cpu().numpy(), g.abs().sum(dim=0).cpu().numpy()
+        _assert_within(gb[e], want, _rounded(size, hi - lo, dtype, want), "bias of expert %d" % e)
