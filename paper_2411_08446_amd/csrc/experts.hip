@@ -10,7 +10,11 @@
 //   forward      q = row, p = d_out, k = d_in       Q = x, P = W_e, both contiguous in k
 //   input        q = row, p = d_in,  k = d_out      Q = grad_out contiguous in k, P = W_e contiguous in p
 //   weight       q = d_out, p = d_in, k = row       Q = grad_out contiguous in q, P = x contiguous in p
-// The matrix instruction takes P as its first operand: a lane then holds consecutive p of one q.
+// The matrix instruction takes P as its first operand: a lane then holds runs of 4 consecutive p of one q.
+//
+// A workgroup computes a tile of BQ x BP outputs.  k goes by chunks: 128 bytes of every row of an operand that is
+// contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into one of
+// two buffers while the waves work on the other, one barrier to a chunk.
 #include "kernels.h"
 #include "rows_by_expert.h"
 
@@ -18,164 +22,421 @@ namespace lshmoe {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 64, kChunk = 32;   // outputs of a workgroup in either direction, k per step
+constexpr int kChunkBytes = 128;   // of a row per chunk
+constexpr int kSteps = 4;          // steps of two 16-byte pieces, one per lane half, per chunk
 
-template <typename DT> struct Elem;
-template <> struct Elem<F32> {
-  typedef float type;
-  static __device__ __forceinline__ float widen(float v) { return v; }
-  static __device__ __forceinline__ float narrow(float v) { return v; }
-};
-template <> struct Elem<BF16> {
-  typedef __bf16 type;
-  static __device__ __forceinline__ float widen(__bf16 v) { return (float)v; }
-  static __device__ __forceinline__ __bf16 narrow(float v) { return (__bf16)v; }
-};
-
-template <typename DT> __device__ __forceinline__ void mma(const uint4& a, const uint4& b, f32x4& c);
-template <> __device__ __forceinline__ void mma<BF16>(const uint4& a, const uint4& b, f32x4& c) {
-  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+// c += P Q of one step: 8 elements of k (bf16, one instruction of 16 with the other lane half) or 4 (binary32, four of 2).
+template <typename DT> __device__ __forceinline__ void mma(const u32x4& a, const u32x4& b, f32x16& c);
+template <> __device__ __forceinline__ void mma<BF16>(const u32x4& a, const u32x4& b, f32x16& c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-template <> __device__ __forceinline__ void mma<F32>(const uint4& a, const uint4& b, f32x4& c) {
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+template <> __device__ __forceinline__ void mma<F32>(const u32x4& a, const u32x4& b, f32x16& c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[0]), __uint_as_float(b[0]), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[1]), __uint_as_float(b[1]), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[2]), __uint_as_float(b[2]), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[3]), __uint_as_float(b[3]), c, 0, 0, 0);
 }
 
-template <typename DT> struct Operand {
-  const typename Elem<DT>::type* base;   // element (index 0, k 0) of the tile
-  int64_t index_stride, k_stride;
-  int indices;                           // of the tile that exist
-};
+// 16 bytes per lane from a buffer straight into LDS: lane l's piece lands at dst + 16 l (dst is wave-uniform); a lane whose
+// offset is behind the buffer's end gets zeros.  Inline assembly, because behind the compiler's own builtin every LDS read
+// waits until the load has landed; the caller waits for these loads itself.
+__device__ __forceinline__ void load16_to_lds(const i32x4& buffer, uint32_t offset, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(offset), "s"(dst), "s"(buffer) : "memory", "m0");
+}
 
-// One tile of out = Q P^T; store(q, p, value) takes the results, sum(q, value) the sums of Q over k where wanted.
-template <typename DT, typename Store, typename Sum>
-__device__ __forceinline__ void tile_product(const Operand<DT>& P, const Operand<DT>& Q, int K, bool sums, Store&& store,
-                                             Sum&& sum) {
-  typedef typename Elem<DT>::type T;
-  constexpr int kPiece = 16 / sizeof(T), kPad = kChunk + kPiece;
-  __shared__ __align__(16) T lp[kTile][kPad];
-  __shared__ __align__(16) T lq[kTile][kPad];
-  const int tid = (int)threadIdx.x, lane = tid % 64, wave = tid / 64, r = lane % 16, g = lane / 16;
-  f32x4 acc[4] = {};
-  float total = 0.0f;
-  for (int k0 = 0; k0 < K; k0 += kChunk) {
-    __syncthreads();
-    for (int i = tid; i < kTile * kChunk; i += 256) {
-      const int kp = P.k_stride == 1 ? i % kChunk : i / kTile, ip = P.k_stride == 1 ? i / kChunk : i % kTile;
-      lp[ip][kp] = ip < P.indices && k0 + kp < K ? P.base[ip * P.index_stride + (int64_t)(k0 + kp) * P.k_stride] : (T)0.0f;
-      const int kq = Q.k_stride == 1 ? i % kChunk : i / kTile, iq = Q.k_stride == 1 ? i / kChunk : i % kTile;
-      lq[iq][kq] = iq < Q.indices && k0 + kq < K ? Q.base[iq * Q.index_stride + (int64_t)(k0 + kq) * Q.k_stride] : (T)0.0f;
-    }
-    __syncthreads();
-    for (int s = 0; s < kChunk / (4 * kPiece); ++s) {
-      const uint4 b = *reinterpret_cast<const uint4*>(&lq[16 * wave + r][(4 * s + g) * kPiece]);
+__device__ __forceinline__ i32x4 buffer_of(const char* base, int64_t bytes) {
+  const uint64_t at = (uint64_t)base;
+  const uint32_t size = bytes <= 0 ? 0u : bytes > 0x7fffffff ? 0x7fffffffu : (uint32_t)bytes;
+  return (i32x4){__builtin_amdgcn_readfirstlane((int)(uint32_t)at), __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xffff),
+                 __builtin_amdgcn_readfirstlane((int)size), 0x00020000};
+}
+
+constexpr uint32_t kNowhere = 0x80000000u;   // an offset behind the end of every buffer
+
+// One operand of a tile: B indices, COLUMNS: contiguous in the index and not in k.
+//
+// LDS holds a chunk of rows as [index][8 pieces], piece s of row i in slot s ^ (i / 2 % 8): 16 lanes reading a piece of 16
+// rows cover 256 bytes once.  A chunk of columns is [k][B elements]; the pieces of bf16 are moved by 64 bytes times k % 4
+// (a transposing read takes 32 bytes each of 4 consecutive k, 16 lanes at a time), of binary32 by 128 bytes times k / 4 % 2.
+template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
+  static constexpr int kItem = ItemSize<DT>::value;
+  static constexpr int kChunk = kChunkBytes / kItem;              // k of a chunk
+  static constexpr int kBytes = B * kChunkBytes;                  // LDS of a chunk
+  static constexpr int kLoads = kBytes / (1024 * WAVES);          // instructions of a wave per chunk
+  static constexpr int kRowPieces = COLUMNS ? B * kItem / 16 : 8; // pieces of a line of LDS
+  static_assert(kLoads * 1024 * WAVES == kBytes, "whole instructions");
+
+  const char* base;       // the tile's first element, chunk 0
+  int64_t bytes;          // from there to the end of what may be read
+  int64_t chunk_step;     // bytes from one chunk to the next
+  uint32_t offset[kLoads];
+  uint32_t k_piece;       // rows: the lane's piece within the chunk, in bytes
+
+  // element (index i, k) is at first + i * stride + k * item (rows) or first + k * stride + i * item (columns); `indices` of the
+  // tile and K of k exist; columns: a line has `line` bytes behind the tile's first index
+  __device__ __forceinline__ Operand(const char* first, uint32_t stride, int indices, int64_t K) {
+    const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
+    base = first;
+    k_piece = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        mma<DT>(*reinterpret_cast<const uint4*>(&lp[16 * i + r][(4 * s + g) * kPiece]), b, acc[i]);
+    for (int i = 0; i < kLoads; ++i) {
+      const int slot = (i * WAVES + wave) * 64 + lane, line = slot / kRowPieces, s = slot % kRowPieces;
+      if (COLUMNS) {
+        const int shift = kItem == 2 ? (line & 3) << 2 : (line >> 2 & 1) << 3;
+        offset[i] = (uint32_t)line * stride + (uint32_t)(s ^ shift) * 16;
+      } else {
+        k_piece = (uint32_t)(s ^ (line >> 1 & 7)) * 16;           // the same for every i: lines are 8 WAVES apart
+        offset[i] = (uint32_t)line * stride + k_piece;
+      }
     }
-    if (sums && tid < kTile)
-      for (int k = 0; k < kChunk; ++k) total += Elem<DT>::widen(lq[tid][k]);
+    if (COLUMNS) {
+      bytes = K == 0 ? 0 : (K - 1) * (int64_t)stride + indices * kItem;
+      chunk_step = (int64_t)kChunk * stride;
+    } else {
+      bytes = indices == 0 ? 0 : (int64_t)(indices - 1) * stride + K * kItem;
+      chunk_step = kChunkBytes;
+    }
   }
-  const int q = 16 * wave + r;
+
+  // Starts the loads of the next chunk into lds; k_bytes: what is left of a row.
+  __device__ __forceinline__ void load(uint32_t lds, int64_t k_bytes) {
+    const uint32_t dst = lds + (uint32_t)((int)threadIdx.x / 64) * 1024;
+    i32x4 buffer = buffer_of(base, bytes);
+    asm volatile("s_nop 4" : "+s"(buffer));    // the descriptor may come from vector instructions: five cycles before its use
+    const bool cut = !COLUMNS && (int64_t)k_piece >= k_bytes;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kLoads; ++i)
+      load16_to_lds(buffer, cut ? kNowhere : offset[i], __builtin_amdgcn_readfirstlane(dst + i * WAVES * 1024));
+    base += chunk_step;
+    bytes -= chunk_step;
+  }
+};
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Fragments of a wave: T tiles of 32 indices from `first` on.
+template <typename DT, bool COLUMNS, int B, int T> struct Fragments {
+  static constexpr int kLine = B * ItemSize<DT>::value;   // columns: bytes of a line
+  static constexpr int kAddresses = COLUMNS ? T : kSteps;
+  uint32_t at[kAddresses];
+
+  __device__ __forceinline__ explicit Fragments(int first) {
+    const int lane = (int)threadIdx.x % 64, r = lane % 32, h = lane / 32;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int p = 16 * i + 4 * g + j;
-      if (q < Q.indices && p < P.indices) store(q, p, acc[i][j]);
+    for (int i = 0; i < kAddresses; ++i) {
+      if (!COLUMNS) {
+        at[i] = (uint32_t)((first + r) * kChunkBytes + ((2 * i + h) ^ (r >> 1 & 7)) * 16);
+      } else if (ItemSize<DT>::value == 2) {
+        // lane l of 16 supplies 8 bytes of k l / 4 and receives 4 k of index l % 16
+        const int kk = lane % 16 / 4;
+        at[i] = (uint32_t)((8 * h + kk) * kLine + ((first / 32 + i) ^ kk) * 64 + (lane / 16 & 1) * 32 + lane % 4 * 8);
+      } else {
+        at[i] = (uint32_t)(4 * h * kLine + ((first / 32 + i) ^ h) * 128 + r * 4);
+      }
     }
-  if (sums && tid < kTile && tid < Q.indices) sum(tid, total);
+  }
+
+  // Fragment of step s (a constant) of tile t.
+  __device__ __forceinline__ u32x4 read(lds_char* lds, int s, int t) const {
+    if (!COLUMNS) return *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(lds + at[s] + t * 32 * kChunkBytes);
+    if (ItemSize<DT>::value == 2) {
+      lds_char* p = lds + at[COLUMNS ? t : 0] + s * 16 * kLine;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + 4 * kLine));
+      const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+      return (u32x4){a.x, a.y, b.x, b.y};
+    }
+    typedef __attribute__((address_space(3))) const uint32_t* word;
+    lds_char* p = lds + at[COLUMNS ? t : 0] + s * 8 * kLine;
+    return (u32x4){*(word)p, *(word)(p + kLine), *(word)(p + 2 * kLine), *(word)(p + 3 * kLine)};
+  }
+};
+
+template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, int WQ> struct Tile {
+  static constexpr int kWaves = WP * WQ, kThreads = 64 * kWaves;
+  static constexpr int TP = BP / WP / 32, TQ = BQ / WQ / 32;     // 32 x 32 tiles of a wave
+  typedef Operand<DT, P_COLUMNS, BP, kWaves> OpP;
+  typedef Operand<DT, Q_COLUMNS, BQ, kWaves> OpQ;
+  static constexpr int kBuffer = OpP::kBytes + OpQ::kBytes;
+  static constexpr size_t kLds = 2 * (size_t)kBuffer;
+
+  f32x16 acc[TP][TQ];
+  f32x16 sums[TQ];          // Q summed over k, where wanted
+
+  // K: elements of k.  SUMS: also the sums of Q over k.
+  template <bool SUMS> __device__ __forceinline__ void run(OpP& P, OpQ& Q, int64_t K) {
+    extern __shared__ uint4 lds[];
+    lds_char* const base = (lds_char*)lds;
+    const uint32_t lds_at = (uint32_t)(uintptr_t)base;
+    const int wave = (int)threadIdx.x / 64;
+    const Fragments<DT, P_COLUMNS, BP, TP> fp(wave % WP * TP * 32);
+    const Fragments<DT, Q_COLUMNS, BQ, TQ> fq(wave / WP * TQ * 32);
+#pragma unroll
+    for (int u = 0; u < TQ; ++u) {
+#pragma unroll
+      for (int t = 0; t < TP; ++t) acc[t][u] = (f32x16){};
+      sums[u] = (f32x16){};
+    }
+    const uint32_t one = std::is_same<DT, BF16>::value ? 0x3f803f80u : 0x3f800000u;
+    const u32x4 ones = {one, one, one, one};
+    int64_t left = K * ItemSize<DT>::value;      // bytes of k whose loads are to be started
+    if (left <= 0) return;
+    P.load(lds_at, left);
+    Q.load(lds_at + OpP::kBytes, left);
+    left -= kChunkBytes;
+    const int chunks = (int)((K + OpP::kChunk - 1) / OpP::kChunk);
+    for (int c = 0; c < chunks; ++c) {
+      // this wave's share of chunk c has landed; behind the barrier everyone's has, and the other buffer is free
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" : : : "memory");
+      if (c + 1 < chunks) {
+        const uint32_t next = lds_at + (c + 1 & 1) * kBuffer;
+        P.load(next, left);
+        Q.load(next + OpP::kBytes, left);
+        left -= kChunkBytes;
+      }
+      lds_char* const now = base + (c & 1) * kBuffer;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        u32x4 a[TP], b[TQ];
+#pragma unroll
+        for (int t = 0; t < TP; ++t) a[t] = fp.read(now, s, t);
+#pragma unroll
+        for (int u = 0; u < TQ; ++u) b[u] = fq.read(now + OpP::kBytes, s, u);
+#pragma unroll
+        for (int t = 0; t < TP; ++t)
+#pragma unroll
+          for (int u = 0; u < TQ; ++u) mma<DT>(a[t], b[u], acc[t][u]);
+        if (SUMS)
+#pragma unroll
+          for (int u = 0; u < TQ; ++u) mma<DT>(ones, b[u], sums[u]);
+      }
+    }
+  }
+
+  // f(q, p, v): the four results p .. p + 3 of q, relative to the tile.
+  template <typename F> __device__ __forceinline__ void each(F&& f) const {
+    const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 32, h = lane / 32;
+#pragma unroll
+    for (int u = 0; u < TQ; ++u)
+#pragma unroll
+      for (int t = 0; t < TP; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v[4] = {acc[t][u][4 * j], acc[t][u][4 * j + 1], acc[t][u][4 * j + 2], acc[t][u][4 * j + 3]};
+          f((wave / WP * TQ + u) * 32 + r, (wave % WP * TP + t) * 32 + 8 * j + 4 * h, v);
+        }
+  }
+};
+
+// Four consecutive elements.
+template <typename DT> struct Four;
+template <> struct Four<F32> {
+  static __device__ __forceinline__ void load(const char* p, float (&v)[4]) {
+    const float4 q = *reinterpret_cast<const float4*>(p);
+    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+  }
+  static __device__ __forceinline__ void store(char* p, const float (&v)[4]) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+};
+template <> struct Four<BF16> {
+  static __device__ __forceinline__ void load(const char* p, float (&v)[4]) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xffff0000u);
+    v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(char* p, const float (&v)[4]) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(f32_to_bf16_pair(v[0], v[1]), f32_to_bf16_pair(v[2], v[3]));
+  }
+};
+
+// Tile number of a workgroup out of `total`: workgroups go round the 8 XCDs, each XCD gets consecutive tiles, so that what
+// neighbouring tiles share is fetched into one L2.  -1: there is none left for it.
+__device__ __forceinline__ int64_t tile_of_block(uint64_t block, int64_t total) {
+  const int64_t per = (total + 7) / 8, slot = (int64_t)(block / 8), n = (int64_t)(block % 8) * per + slot;
+  return slot < per && n < total ? n : -1;
+}
+inline uint64_t blocks_for(uint64_t tiles) { return (tiles + 7) / 8 * 8; }
+
+template <typename DT, typename TILE, int BP, int BQ>
+__global__ __launch_bounds__(TILE::kThreads) void forward_kernel(const char* __restrict__ x, const char* __restrict__ w,
+                                                                 const char* __restrict__ bias,
+                                                                 const int32_t* __restrict__ offsets, int64_t rows, int d_in,
+                                                                 int d_out, int E, int act, char* __restrict__ pre,
+                                                                 char* __restrict__ out) {
+  constexpr int kItem = ItemSize<DT>::value;
+  const RowTiles tiles(offsets, E, rows, BQ);
+  const int ptiles = (d_out + BP - 1) / BP;
+  const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
+  if (n < 0) return;
+  const RowTile rt = tiles.find(n / ptiles);
+  const int p0 = (int)(n % ptiles) * BP, np = min(BP, d_out - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
+  typename TILE::OpP P(w + ((int64_t)rt.expert * d_out + p0) * d_in * kItem, (uint32_t)d_in * kItem, np, d_in);
+  typename TILE::OpQ Q(x + rt.first * d_in * kItem, (uint32_t)d_in * kItem, nq, d_in);
+  TILE tile;
+  tile.template run<false>(P, Q, d_in);
+  tile.each([&](int q, int p, const float (&v)[4]) {
+    if (q >= nq || p >= np) return;
+    float y[4] = {v[0], v[1], v[2], v[3]};
+    if (bias) {
+      float b[4];
+      Four<DT>::load(bias + ((int64_t)rt.expert * d_out + p0 + p) * kItem, b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] += b[i];
+    }
+    const int64_t at = ((rt.first + q) * d_out + p0 + p) * kItem;
+    if (pre) Four<DT>::store(pre + at, y);
+    if (act != LSHMOE_ACT_NONE)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = activate(y[i], act);
+    Four<DT>::store(out + at, y);
+  });
 }
 
-template <typename DT>
-__global__ __launch_bounds__(256) void forward_kernel(const void* x, const void* w, const void* bias,
-                                                      const int32_t* __restrict__ offsets, int64_t rows, int d_in, int d_out,
-                                                      int E, int act, void* pre, void* out) {
-  typedef typename Elem<DT>::type T;
-  const RowTile t = find_row_tile(offsets, E, rows, kTile, (int64_t)linear_block() / ((d_out + kTile - 1) / kTile));
-  if (t.expert < 0) return;
-  const int p0 = (int)(linear_block() % ((d_out + kTile - 1) / kTile)) * kTile;
-  const Operand<DT> Q = {(const T*)x + t.first * d_in, d_in, 1, (int)min((int64_t)kTile, t.end - t.first)};
-  const Operand<DT> P = {(const T*)w + ((int64_t)t.expert * d_out + p0) * d_in, d_in, 1, min(kTile, d_out - p0)};
-  tile_product<DT>(P, Q, d_in, false, [&](int q, int p, float v) {
-    if (bias) v += Elem<DT>::widen(((const T*)bias)[(int64_t)t.expert * d_out + p0 + p]);
-    const int64_t at = (t.first + q) * d_out + p0 + p;
-    if (pre) ((T*)pre)[at] = Elem<DT>::narrow(v);
-    ((T*)out)[at] = Elem<DT>::narrow(activate(v, act));
-  }, [](int, float) {});
+template <typename DT, typename TILE, int BP, int BQ>
+__global__ __launch_bounds__(TILE::kThreads) void input_grad_kernel(const char* __restrict__ grad_out,
+                                                                    const char* __restrict__ w,
+                                                                    const int32_t* __restrict__ offsets, int64_t rows,
+                                                                    int d_in, int d_out, int E, int act,
+                                                                    const char* __restrict__ pre, char* __restrict__ grad_x) {
+  constexpr int kItem = ItemSize<DT>::value;
+  const RowTiles tiles(offsets, E, rows, BQ);
+  const int ptiles = (d_in + BP - 1) / BP;
+  const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
+  if (n < 0) return;
+  const RowTile rt = tiles.find(n / ptiles);
+  const int p0 = (int)(n % ptiles) * BP, np = min(BP, d_in - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
+  typename TILE::OpP P(w + ((int64_t)rt.expert * d_out * d_in + p0) * kItem, (uint32_t)d_in * kItem, np, d_out);
+  typename TILE::OpQ Q(grad_out + rt.first * d_out * kItem, (uint32_t)d_out * kItem, nq, d_out);
+  TILE tile;
+  tile.template run<false>(P, Q, d_out);
+  tile.each([&](int q, int p, const float (&v)[4]) {
+    if (q >= nq || p >= np) return;
+    float y[4] = {v[0], v[1], v[2], v[3]};
+    const int64_t at = ((rt.first + q) * d_in + p0 + p) * kItem;
+    if (act != LSHMOE_ACT_NONE) {
+      float b[4];
+      Four<DT>::load(pre + at, b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] *= activation_slope(b[i], act);
+    }
+    Four<DT>::store(grad_x + at, y);
+  });
 }
 
-template <typename DT>
-__global__ __launch_bounds__(256) void input_grad_kernel(const void* grad_out, const void* w,
-                                                         const int32_t* __restrict__ offsets, int64_t rows, int d_in,
-                                                         int d_out, int E, int act, const void* pre, void* grad_x) {
-  typedef typename Elem<DT>::type T;
-  const RowTile t = find_row_tile(offsets, E, rows, kTile, (int64_t)linear_block() / ((d_in + kTile - 1) / kTile));
-  if (t.expert < 0) return;
-  const int p0 = (int)(linear_block() % ((d_in + kTile - 1) / kTile)) * kTile;
-  const Operand<DT> Q = {(const T*)grad_out + t.first * d_out, d_out, 1, (int)min((int64_t)kTile, t.end - t.first)};
-  const Operand<DT> P = {(const T*)w + (int64_t)t.expert * d_out * d_in + p0, 1, d_in, min(kTile, d_in - p0)};
-  tile_product<DT>(P, Q, d_out, false, [&](int q, int p, float v) {
-    const int64_t at = (t.first + q) * d_in + p0 + p;
-    if (act != LSHMOE_ACT_NONE) v *= activation_slope(Elem<DT>::widen(((const T*)pre)[at]), act);
-    ((T*)grad_x)[at] = Elem<DT>::narrow(v);
-  }, [](int, float) {});
-}
-
-template <typename DT>
-__global__ __launch_bounds__(256) void weight_grad_kernel(const void* grad_out, const void* x,
-                                                          const int32_t* __restrict__ offsets, int64_t rows, int d_in,
-                                                          int d_out, void* grad_w, void* grad_bias) {
-  typedef typename Elem<DT>::type T;
-  const int ptiles = (d_in + kTile - 1) / kTile, qtiles = (d_out + kTile - 1) / kTile;
-  const uint64_t block = linear_block();
-  const int64_t e = block / ((uint64_t)ptiles * qtiles);
-  const int p0 = (int)(block % ptiles) * kTile, q0 = (int)(block / ptiles % qtiles) * kTile;
+template <typename DT, typename TILE, int BP, int BQ>
+__global__ __launch_bounds__(TILE::kThreads) void weight_grad_kernel(const char* __restrict__ grad_out,
+                                                                     const char* __restrict__ x,
+                                                                     const int32_t* __restrict__ offsets, int64_t rows,
+                                                                     int d_in, int d_out, int E, char* __restrict__ grad_w,
+                                                                     char* __restrict__ grad_bias) {
+  constexpr int kItem = ItemSize<DT>::value;
+  const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ;
+  const int64_t n = tile_of_block(linear_block(), (int64_t)E * ptiles * qtiles);
+  if (n < 0) return;
+  const int64_t e = n / ((int64_t)ptiles * qtiles);
+  const int p0 = (int)(n % ptiles) * BP, q0 = (int)(n / ptiles % qtiles) * BQ;
+  const int np = min(BP, d_in - p0), nq = min(BQ, d_out - q0);
   const RowRange range = rows_of(offsets, (int)e, rows);
-  const Operand<DT> Q = {(const T*)grad_out + range.lo * d_out + q0, 1, d_out, min(kTile, d_out - q0)};
-  const Operand<DT> P = {(const T*)x + range.lo * d_in + p0, 1, d_in, min(kTile, d_in - p0)};
-  tile_product<DT>(P, Q, (int)(range.hi - range.lo), grad_bias != nullptr && p0 == 0, [&](int q, int p, float v) {
-    ((T*)grad_w)[((int64_t)e * d_out + q0 + q) * d_in + p0 + p] = Elem<DT>::narrow(v);
-  }, [&](int q, float v) { ((T*)grad_bias)[(int64_t)e * d_out + q0 + q] = Elem<DT>::narrow(v); });
+  const int64_t K = range.hi - range.lo;
+  typename TILE::OpP P(x + (range.lo * d_in + p0) * kItem, (uint32_t)d_in * kItem, np, K);
+  typename TILE::OpQ Q(grad_out + (range.lo * d_out + q0) * kItem, (uint32_t)d_out * kItem, nq, K);
+  TILE tile;
+  const bool sums = grad_bias != nullptr && p0 == 0;
+  if (sums)
+    tile.template run<true>(P, Q, K);
+  else
+    tile.template run<false>(P, Q, K);
+  tile.each([&](int q, int p, const float (&v)[4]) {
+    if (q < nq && p < np) Four<DT>::store(grad_w + ((e * d_out + q0 + q) * d_in + p0 + p) * kItem, v);
+  });
+  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
+  if (sums && wave % (BP / 32 / TILE::TP) == 0 && lane < 32) {
+#pragma unroll
+    for (int u = 0; u < TILE::TQ; ++u) {
+      const int q = (wave / (BP / 32 / TILE::TP) * TILE::TQ + u) * 32 + lane;
+      if (q >= nq) continue;
+      const float v = tile.sums[u][0];
+      if (kItem == 4) reinterpret_cast<float*>(grad_bias)[e * d_out + q0 + q] = v;
+      else reinterpret_cast<__bf16*>(grad_bias)[e * d_out + q0 + q] = (__bf16)v;
+    }
+  }
+}
+
+template <typename DT> struct Shape { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4; };
+template <> struct Shape<F32> { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2; };
+
+// More than 64 KB of LDS has to be asked for, once per kernel and device; asking again is harmless.
+template <typename K> hipError_t allow_lds(K kernel, size_t bytes) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <typename DT>
+hipError_t forward(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out,
+                   int E, int act, void* pre, void* out, hipStream_t stream) {
+  typedef Shape<DT> S;
+  typedef Tile<DT, false, false, S::BP, S::BQ, S::WP, S::WQ> TILE;
+  auto kernel = forward_kernel<DT, TILE, S::BP, S::BQ>;
+  if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
+  const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, S::BQ) * ((d_out + S::BP - 1) / S::BP);
+  kernel<<<grid_of_blocks(blocks_for(tiles)), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)x, (const char*)w, (const char*)bias, offsets, rows, d_in, d_out, E, act, (char*)pre, (char*)out);
+  return hipGetLastError();
+}
+
+template <typename DT>
+hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
+                      int act, const void* pre, void* grad_x, hipStream_t stream) {
+  typedef Shape<DT> S;
+  typedef Tile<DT, true, false, S::BP, S::BQ, S::WP, S::WQ> TILE;
+  auto kernel = input_grad_kernel<DT, TILE, S::BP, S::BQ>;
+  if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
+  const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, S::BQ) * ((d_in + S::BP - 1) / S::BP);
+  kernel<<<grid_of_blocks(blocks_for(tiles)), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)grad_out, (const char*)w, offsets, rows, d_in, d_out, E, act, (const char*)pre, (char*)grad_x);
+  return hipGetLastError();
+}
+
+template <typename DT>
+hipError_t weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
+                       void* grad_w, void* grad_bias, hipStream_t stream) {
+  typedef Shape<DT> S;
+  typedef Tile<DT, true, true, S::BP, S::BQ, S::WP, S::WQ> TILE;
+  auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ>;
+  if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
+  const uint64_t tiles = (uint64_t)E * ((d_in + S::BP - 1) / S::BP) * ((d_out + S::BQ - 1) / S::BQ);
+  kernel<<<grid_of_blocks(blocks_for(tiles)), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)grad_out, (const char*)x, offsets, rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_expert_forward(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows,
                                  int d_in, int d_out, int E, bool bf16, int act, void* pre, void* out, hipStream_t stream) {
-  const dim3 grid = grid_of_blocks((uint64_t)most_row_tiles(rows, E, kTile) * ((d_out + kTile - 1) / kTile));
-  if (bf16)
-    forward_kernel<BF16><<<grid, 256, 0, stream>>>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out);
-  else
-    forward_kernel<F32><<<grid, 256, 0, stream>>>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out);
-  return hipGetLastError();
+  return bf16 ? forward<BF16>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out, stream)
+              : forward<F32>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out, stream);
 }
 
 hipError_t launch_expert_input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in,
                                     int d_out, int E, bool bf16, int act, const void* pre, void* grad_x, hipStream_t stream) {
-  const dim3 grid = grid_of_blocks((uint64_t)most_row_tiles(rows, E, kTile) * ((d_in + kTile - 1) / kTile));
-  if (bf16)
-    input_grad_kernel<BF16><<<grid, 256, 0, stream>>>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x);
-  else
-    input_grad_kernel<F32><<<grid, 256, 0, stream>>>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x);
-  return hipGetLastError();
+  return bf16 ? input_grad<BF16>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream)
+              : input_grad<F32>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
 }
 
 size_t expert_workspace_bytes(int64_t, int, int, int, bool) { return 0; }
 
 hipError_t launch_expert_weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in,
                                      int d_out, int E, bool bf16, void* grad_w, void* grad_bias, char*, hipStream_t stream) {
-  const dim3 grid = grid_of_blocks((uint64_t)E * ((d_in + kTile - 1) / kTile) * ((d_out + kTile - 1) / kTile));
-  if (bf16)
-    weight_grad_kernel<BF16><<<grid, 256, 0, stream>>>(grad_out, x, offsets, rows, d_in, d_out, grad_w, grad_bias);
-  else
-    weight_grad_kernel<F32><<<grid, 256, 0, stream>>>(grad_out, x, offsets, rows, d_in, d_out, grad_w, grad_bias);
-  return hipGetLastError();
+  return bf16 ? weight_grad<BF16>(grad_out, x, offsets, rows, d_in, d_out, E, grad_w, grad_bias, stream)
+              : weight_grad<F32>(grad_out, x, offsets, rows, d_in, d_out, E, grad_w, grad_bias, stream);
 }
 
 }  // namespace lshmoe

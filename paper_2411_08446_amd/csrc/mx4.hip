@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) void forward_kernel(const char* __restrict__ x
                                                       const void* bias, const int32_t* __restrict__ offsets, int64_t rows,
                                                       int d_in, int d_out, int E, int act, void* out) {
   const int ptiles = (d_out + kTile - 1) / kTile;
-  const RowTile t = find_row_tile(offsets, E, rows, kTile, (int64_t)linear_block() / ptiles);
+  const RowTile t = RowTiles(offsets, E, rows, kTile).find((int64_t)linear_block() / ptiles);
   if (t.expert < 0) return;
   const int p0 = (int)(linear_block() % ptiles) * kTile;
   const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 16, g = lane / 16;

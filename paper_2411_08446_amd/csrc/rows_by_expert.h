@@ -23,36 +23,63 @@ __device__ __forceinline__ RowRange rows_of(const int32_t* __restrict__ offsets,
 inline int64_t most_row_tiles(int64_t rows, int E, int tile) { return rows / tile + (E < rows ? E : rows); }
 
 struct RowTile {
-  int expert;           // -1: there are fewer row tiles than that
+  int expert;           // -1: there is no such tile
   int64_t first, end;   // its first row, the end of its expert's rows
 };
 
-// Row tile number m of all experts' row tiles, in the order of the experts.  Every wave finds it by itself: lane e % 64 counts
-// expert e's tiles and the counts are summed over the lanes.
-__device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ offsets, int E, int64_t rows, int tile, int64_t m) {
-  const int lane = (int)threadIdx.x % kWave;
-  int64_t before = 0;                         // tiles of the experts below e0
-  for (int e0 = 0; e0 < E; e0 += kWave) {
+// The experts' row tiles of `tile` rows, in the order of the experts.  Every wave counts them by itself: lane e % 64 has expert
+// e's, summed over the lanes.  The first 64 experts' counts stay in registers.
+struct RowTiles {
+  const int32_t* offsets;
+  int64_t rows;
+  int E, tile;
+  int lo, hi, upto;     // of expert `lane`: its rows, the tiles up to and with it
+  int64_t total;
+
+  __device__ __forceinline__ void count(int e0, int& lo_, int& hi_, int& upto_) const {
+    const int lane = (int)threadIdx.x % kWave;
     RowRange range = {0, 0};
     if (e0 + lane < E) range = rows_of(offsets, e0 + lane, rows);
-    const int tiles = (int)((range.hi - range.lo + tile - 1) / tile);
-    int upto = tiles;
+    lo_ = (int)range.lo;
+    hi_ = (int)range.hi;
+    upto_ = (hi_ - lo_ + tile - 1) / tile;
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) {
-      const int below = __shfl_up(upto, s, kWave);
-      if (lane >= s) upto += below;
+      const int below = __shfl_up(upto_, s, kWave);
+      if (lane >= s) upto_ += below;
     }
-    const uint64_t past = __ballot(before + upto > m);
-    if (past != 0) {
-      const int at = __ffsll((unsigned long long)past) - 1;
-      const int lo = __builtin_amdgcn_readlane((int)range.lo, at), hi = __builtin_amdgcn_readlane((int)range.hi, at);
-      const int64_t skipped = m - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at));
-      return {e0 + at, lo + skipped * tile, hi};
-    }
-    before += __builtin_amdgcn_readlane(upto, kWave - 1);
   }
-  return {-1, 0, 0};
-}
+
+  __device__ __forceinline__ RowTiles(const int32_t* __restrict__ offsets_, int E_, int64_t rows_, int tile_)
+      : offsets(offsets_), rows(rows_), E(E_), tile(tile_) {
+    count(0, lo, hi, upto);
+    total = __builtin_amdgcn_readlane(upto, kWave - 1);
+    for (int e0 = kWave; e0 < E; e0 += kWave) {
+      int l, h, u;
+      count(e0, l, h, u);
+      total += __builtin_amdgcn_readlane(u, kWave - 1);
+    }
+  }
+
+  __device__ __forceinline__ RowTile find(int64_t m) const {
+    int64_t before = 0;                       // tiles of the experts below e0
+    int l = lo, h = hi, u = upto;
+    for (int e0 = 0;;) {
+      const uint64_t past = __ballot(before + u > m);
+      if (past != 0) {
+        const int at = __ffsll((unsigned long long)past) - 1;
+        const int rlo = __builtin_amdgcn_readlane(l, at), rhi = __builtin_amdgcn_readlane(h, at);
+        const int upto_at = __builtin_amdgcn_readlane(u, at);
+        const int64_t skipped = m - before - (upto_at - (rhi - rlo + tile - 1) / tile);
+        return {e0 + at, rlo + skipped * tile, rhi};
+      }
+      before += __builtin_amdgcn_readlane(u, kWave - 1);
+      e0 += kWave;
+      if (e0 >= E) return {-1, 0, 0};
+      count(e0, l, h, u);
+    }
+  }
+};
 
 __device__ __forceinline__ float activate(float v, int act) {
   if (act == LSHMOE_ACT_RELU) return v > 0.0f || v != v ? v : 0.0f;
