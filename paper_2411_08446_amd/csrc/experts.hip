@@ -220,40 +220,40 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     }
   }
 
-  // f(q, p, v): the four results p .. p + 3 of q, relative to the tile.
-  template <typename F> __device__ __forceinline__ void each(F&& f) const {
+  // f(q, p, v): a piece's worth of results of q from p on, relative to the tile.  A wave's results go through LDS, binary32, 32 q
+  // at a time, so that the 16 bytes that a lane reads and writes of the outputs are next to its neighbours': 256 bytes
+  // of an output row at a time instead of 16.  Slots of 16 bytes are moved by the row against bank conflicts.
+  template <typename F> __device__ __forceinline__ void finish(F&& f) const {
+    constexpr int kElems = Piece<DT>::kElems, kRow = TP * 32 * 4, kLanes = TP * 32 / kElems;
+    static_assert(kWaves * 32 * kRow <= (int)kLds && kRow % 256 == 0, "the waves' parts fit");
+    extern __shared__ uint4 lds[];
     const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 32, h = lane / 32;
+    char* const part = reinterpret_cast<char*>(lds) + wave * 32 * kRow;
+    __syncthreads();               // the other waves are done with the last chunk
 #pragma unroll
-    for (int u = 0; u < TQ; ++u)
+    for (int u = 0; u < TQ; ++u) {
 #pragma unroll
       for (int t = 0; t < TP; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float v[4] = {acc[t][u][4 * j], acc[t][u][4 * j + 1], acc[t][u][4 * j + 2], acc[t][u][4 * j + 3]};
-          f((wave / WP * TQ + u) * 32 + r, (wave % WP * TP + t) * 32 + 8 * j + 4 * h, v);
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<float4*>(part + r * kRow + ((8 * t + 2 * j + h) ^ (r & 15)) * 16) =
+              make_float4(acc[t][u][4 * j], acc[t][u][4 * j + 1], acc[t][u][4 * j + 2], acc[t][u][4 * j + 3]);
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("" : : : "memory");
+#pragma unroll
+      for (int i = 0; i < 32 * kLanes / 64; ++i) {
+        const int q = i * (64 / kLanes) + lane / kLanes, c = lane % kLanes;
+        float v[kElems];
+#pragma unroll
+        for (int j = 0; j < kElems / 4; ++j) {
+          const float4 w = *reinterpret_cast<const float4*>(part + q * kRow + ((c * (kElems / 4) + j) ^ (q & 15)) * 16);
+          v[4 * j] = w.x; v[4 * j + 1] = w.y; v[4 * j + 2] = w.z; v[4 * j + 3] = w.w;
         }
-  }
-};
-
-// Four consecutive elements.
-template <typename DT> struct Four;
-template <> struct Four<F32> {
-  static __device__ __forceinline__ void load(const char* p, float (&v)[4]) {
-    const float4 q = *reinterpret_cast<const float4*>(p);
-    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-  }
-  static __device__ __forceinline__ void store(char* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
-};
-template <> struct Four<BF16> {
-  static __device__ __forceinline__ void load(const char* p, float (&v)[4]) {
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
-    v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xffff0000u);
-    v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xffff0000u);
-  }
-  static __device__ __forceinline__ void store(char* p, const float (&v)[4]) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(f32_to_bf16_pair(v[0], v[1]), f32_to_bf16_pair(v[2], v[3]));
+        f((wave / WP * TQ + u) * 32 + q, wave % WP * TP * 32 + c * kElems, v);
+      }
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("" : : : "memory");
+    }
   }
 };
 
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(TILE::kThreads) void forward_kernel(const char* __r
                                                                  const int32_t* __restrict__ offsets, int64_t rows, int d_in,
                                                                  int d_out, int E, int act, char* __restrict__ pre,
                                                                  char* __restrict__ out) {
-  constexpr int kItem = ItemSize<DT>::value;
+  constexpr int kItem = ItemSize<DT>::value, kElems = Piece<DT>::kElems;
   const RowTiles tiles(offsets, E, rows, BQ);
   const int ptiles = (d_out + BP - 1) / BP;
   const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
@@ -282,21 +282,20 @@ __global__ __launch_bounds__(TILE::kThreads) void forward_kernel(const char* __r
   typename TILE::OpQ Q(x + rt.first * d_in * kItem, (uint32_t)d_in * kItem, nq, d_in);
   TILE tile;
   tile.template run<false>(P, Q, d_in);
-  tile.each([&](int q, int p, const float (&v)[4]) {
+  tile.finish([&](int q, int p, float (&v)[kElems]) {
     if (q >= nq || p >= np) return;
-    float y[4] = {v[0], v[1], v[2], v[3]};
     if (bias) {
-      float b[4];
-      Four<DT>::load(bias + ((int64_t)rt.expert * d_out + p0 + p) * kItem, b);
+      float b[kElems];
+      Piece<DT>::widen(load16(bias + ((int64_t)rt.expert * d_out + p0 + p) * kItem), b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] += b[i];
+      for (int i = 0; i < kElems; ++i) v[i] += b[i];
     }
     const int64_t at = ((rt.first + q) * d_out + p0 + p) * kItem;
-    if (pre) Four<DT>::store(pre + at, y);
+    if (pre) store16(pre + at, Piece<DT>::narrow(v));
     if (act != LSHMOE_ACT_NONE)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = activate(y[i], act);
-    Four<DT>::store(out + at, y);
+      for (int i = 0; i < kElems; ++i) v[i] = activate(v[i], act);
+    store16(out + at, Piece<DT>::narrow(v));
   });
 }
 
@@ -306,7 +305,7 @@ __global__ __launch_bounds__(TILE::kThreads) void input_grad_kernel(const char* 
                                                                     const int32_t* __restrict__ offsets, int64_t rows,
                                                                     int d_in, int d_out, int E, int act,
                                                                     const char* __restrict__ pre, char* __restrict__ grad_x) {
-  constexpr int kItem = ItemSize<DT>::value;
+  constexpr int kItem = ItemSize<DT>::value, kElems = Piece<DT>::kElems;
   const RowTiles tiles(offsets, E, rows, BQ);
   const int ptiles = (d_in + BP - 1) / BP;
   const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
@@ -317,17 +316,16 @@ __global__ __launch_bounds__(TILE::kThreads) void input_grad_kernel(const char* 
   typename TILE::OpQ Q(grad_out + rt.first * d_out * kItem, (uint32_t)d_out * kItem, nq, d_out);
   TILE tile;
   tile.template run<false>(P, Q, d_out);
-  tile.each([&](int q, int p, const float (&v)[4]) {
+  tile.finish([&](int q, int p, float (&v)[kElems]) {
     if (q >= nq || p >= np) return;
-    float y[4] = {v[0], v[1], v[2], v[3]};
     const int64_t at = ((rt.first + q) * d_in + p0 + p) * kItem;
     if (act != LSHMOE_ACT_NONE) {
-      float b[4];
-      Four<DT>::load(pre + at, b);
+      float b[kElems];
+      Piece<DT>::widen(load16(pre + at), b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] *= activation_slope(b[i], act);
+      for (int i = 0; i < kElems; ++i) v[i] *= activation_slope(b[i], act);
     }
-    Four<DT>::store(grad_x + at, y);
+    store16(grad_x + at, Piece<DT>::narrow(v));
   });
 }
 
@@ -354,8 +352,8 @@ __global__ __launch_bounds__(TILE::kThreads) void weight_grad_kernel(const char*
     tile.template run<true>(P, Q, K);
   else
     tile.template run<false>(P, Q, K);
-  tile.each([&](int q, int p, const float (&v)[4]) {
-    if (q < nq && p < np) Four<DT>::store(grad_w + ((e * d_out + q0 + q) * d_in + p0 + p) * kItem, v);
+  tile.finish([&](int q, int p, float (&v)[Piece<DT>::kElems]) {
+    if (q < nq && p < np) store16(grad_w + ((e * d_out + q0 + q) * d_in + p0 + p) * kItem, Piece<DT>::narrow(v));
   });
   const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
   if (sums && wave % (BP / 32 / TILE::TP) == 0 && lane < 32) {
