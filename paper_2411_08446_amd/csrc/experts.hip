@@ -15,6 +15,9 @@
 // A workgroup computes a tile of BQ x BP outputs.  k goes by chunks: 128 bytes of every row of an operand that is
 // contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into one of
 // two buffers while the waves work on the other, one barrier to a chunk.
+#include <type_traits>
+#include <utility>
+
 #include "kernels.h"
 #include "rows_by_expert.h"
 
@@ -28,7 +31,11 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunkBytes = 128;   // of a row per chunk
-constexpr int kSteps = 4;          // steps of two 16-byte pieces, one per lane half, per chunk
+constexpr int kPieces = kChunkBytes / 16;
+constexpr int kSteps = kPieces / 2;   // steps of two 16-byte pieces, one per lane half, per chunk
+
+// Piece s of row i of a chunk of rows lies in slot s ^ row_shift(i): 16 lanes reading a piece of 16 rows cover 256 bytes once.
+__device__ __forceinline__ int row_shift(int i) { return i / (256 / kChunkBytes) % kPieces; }
 
 // c += P Q of one step: 8 elements of k (bf16, one instruction of 16 with the other lane half) or 4 (binary32, four of 2).
 template <typename DT> __device__ __forceinline__ void mma(const u32x4& a, const u32x4& b, f32x16& c);
@@ -60,15 +67,14 @@ constexpr uint32_t kNowhere = 0x80000000u;   // an offset behind the end of ever
 
 // One operand of a tile: B indices, COLUMNS: contiguous in the index and not in k.
 //
-// LDS holds a chunk of rows as [index][8 pieces], piece s of row i in slot s ^ (i / 2 % 8): 16 lanes reading a piece of 16
-// rows cover 256 bytes once.  A chunk of columns is [k][B elements]; the pieces of bf16 are moved by 64 bytes times k % 4
+// LDS holds a chunk of rows as [index][kPieces].  A chunk of columns is [k][B elements]; the pieces of bf16 are moved by 64 bytes times k % 4
 // (a transposing read takes 32 bytes each of 4 consecutive k, 16 lanes at a time), of binary32 by 128 bytes times k / 4 % 2.
 template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
   static constexpr int kItem = ItemSize<DT>::value;
   static constexpr int kChunk = kChunkBytes / kItem;              // k of a chunk
   static constexpr int kBytes = B * kChunkBytes;                  // LDS of a chunk
   static constexpr int kLoads = kBytes / (1024 * WAVES);          // instructions of a wave per chunk
-  static constexpr int kRowPieces = COLUMNS ? B * kItem / 16 : 8; // pieces of a line of LDS
+  static constexpr int kRowPieces = COLUMNS ? B * kItem / 16 : kPieces;   // pieces of a line of LDS
   static_assert(kLoads * 1024 * WAVES == kBytes, "whole instructions");
 
   const char* base;       // the tile's first element, chunk 0
@@ -90,7 +96,7 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
         const int shift = kItem == 2 ? (line & 3) << 2 : (line >> 2 & 1) << 3;
         offset[i] = (uint32_t)line * stride + (uint32_t)(s ^ shift) * 16;
       } else {
-        k_piece = (uint32_t)(s ^ (line >> 1 & 7)) * 16;           // the same for every i: lines are 8 WAVES apart
+        k_piece = (uint32_t)(s ^ row_shift(line)) * 16;           // the same for every i: lines are 8 WAVES apart
         offset[i] = (uint32_t)line * stride + k_piece;
       }
     }
@@ -119,6 +125,14 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
 
 typedef __attribute__((address_space(3))) char lds_char;
 
+// Compile-time loop: f is called with std::integral_constant<int, 0> .. <int, N - 1>.
+template <typename F, int... I> __device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F> __device__ __forceinline__ void static_for(F&& f) {
+  static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
 // Fragments of a wave: T tiles of 32 indices from `first` on.
 template <typename DT, bool COLUMNS, int B, int T> struct Fragments {
   static constexpr int kLine = B * ItemSize<DT>::value;   // columns: bytes of a line
@@ -130,7 +144,7 @@ template <typename DT, bool COLUMNS, int B, int T> struct Fragments {
 #pragma unroll
     for (int i = 0; i < kAddresses; ++i) {
       if (!COLUMNS) {
-        at[i] = (uint32_t)((first + r) * kChunkBytes + ((2 * i + h) ^ (r >> 1 & 7)) * 16);
+        at[i] = (uint32_t)((first + r) * kChunkBytes + ((2 * i + h) ^ row_shift(r)) * 16);
       } else if (ItemSize<DT>::value == 2) {
         // lane l of 16 supplies 8 bytes of k l / 4 and receives 4 k of index l % 16
         const int kk = lane % 16 / 4;
@@ -162,6 +176,7 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
   static constexpr int TP = BP / WP / 32, TQ = BQ / WQ / 32;     // 32 x 32 tiles of a wave
   typedef Operand<DT, P_COLUMNS, BP, kWaves> OpP;
   typedef Operand<DT, Q_COLUMNS, BQ, kWaves> OpQ;
+  static constexpr int kPieceReads = std::is_same<DT, BF16>::value ? 8 : 4;   // bytes that one read of columns gives a lane
   static constexpr int kBuffer = OpP::kBytes + OpQ::kBytes;
   static constexpr size_t kLds = 2 * (size_t)kBuffer;
 
@@ -185,39 +200,61 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     const uint32_t one = std::is_same<DT, BF16>::value ? 0x3f803f80u : 0x3f800000u;
     const u32x4 ones = {one, one, one, one};
     int64_t left = K * ItemSize<DT>::value;      // bytes of k whose loads are to be started
-    if (left <= 0) return;
-    P.load(lds_at, left);
-    Q.load(lds_at + OpP::kBytes, left);
-    left -= kChunkBytes;
     const int chunks = (int)((K + OpP::kChunk - 1) / OpP::kChunk);
+    auto start = [&](int slot) {
+      P.load(lds_at + slot * kBuffer, left);
+      Q.load(lds_at + slot * kBuffer + OpP::kBytes, left);
+      left -= kChunkBytes;
+    };
+    u32x4 a[2][TP], b[2][TQ];        // fragments of a step and of the one after it
+    auto read = [&](int into, lds_char* from, int s) {
+#pragma unroll
+      for (int t = 0; t < TP; ++t) a[into][t] = fp.read(from, s, t);
+#pragma unroll
+      for (int u = 0; u < TQ; ++u) b[into][u] = fq.read(from + OpP::kBytes, s, u);
+    };
+    if (chunks > 0) start(0);
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    if (chunks > 1) start(1);
+    read(0, base, 0);
     for (int c = 0; c < chunks; ++c) {
-      // this wave's share of chunk c has landed; behind the barrier everyone's has, and the other buffer is free
-      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" : : : "memory");
-      if (c + 1 < chunks) {
-        const uint32_t next = lds_at + (c + 1 & 1) * kBuffer;
-        P.load(next, left);
-        Q.load(next + OpP::kBytes, left);
-        left -= kChunkBytes;
-      }
       lds_char* const now = base + (c & 1) * kBuffer;
+      lds_char* const next = base + (~c & 1) * kBuffer;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-        u32x4 a[TP], b[TQ];
-#pragma unroll
-        for (int t = 0; t < TP; ++t) a[t] = fp.read(now, s, t);
-#pragma unroll
-        for (int u = 0; u < TQ; ++u) b[u] = fq.read(now + OpP::kBytes, s, u);
+        // the fragments of the next step are on their way while this one's products run
+        if (s + 1 < kSteps) {
+          read((s + 1) & 1, now, s + 1);
+        } else {
+          // The last fragments of chunk c are in registers, this wave's share of chunk c + 1 has landed.  Behind the barrier that
+          // is so for all waves: chunk c's buffer is free for chunk c + 2, chunk c + 1 may be read.
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" : : : "memory");
+          if (c + 2 < chunks) start(c & 1);
+          read(0, next, 0);
+        }
 #pragma unroll
         for (int t = 0; t < TP; ++t)
 #pragma unroll
-          for (int u = 0; u < TQ; ++u) mma<DT>(a[t], b[u], acc[t][u]);
+          for (int u = 0; u < TQ; ++u) mma<DT>(a[s & 1][t], b[s & 1][u], acc[t][u]);
         if (SUMS)
 #pragma unroll
-          for (int u = 0; u < TQ; ++u) mma<DT>(ones, b[u], sums[u]);
+          for (int u = 0; u < TQ; ++u) mma<DT>(ones, b[s & 1][u], sums[u]);
+        // reads and products take turns
+        constexpr int kReads = TP * (P_COLUMNS ? 16 / kPieceReads : 1) + TQ * (Q_COLUMNS ? 16 / kPieceReads : 1);
+        constexpr int kProducts = (TP * TQ + (SUMS ? TQ : 0)) * (std::is_same<DT, BF16>::value ? 1 : 4);
+        static_for<TP * TQ>([&](auto i) {
+          constexpr int n = decltype(i)::value;
+          __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / (TP * TQ) - kReads * n / (TP * TQ), 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / (TP * TQ) - kProducts * n / (TP * TQ), 0);
+        });
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
   }
 
   // f(q, p, v): a piece's worth of results of q from p on, relative to the tile.  A wave's results go through LDS, binary32, 32 q
@@ -266,7 +303,7 @@ __device__ __forceinline__ int64_t tile_of_block(uint64_t block, int64_t total) 
 inline uint64_t blocks_for(uint64_t tiles) { return (tiles + 7) / 8 * 8; }
 
 template <typename DT, typename TILE, int BP, int BQ>
-__global__ __launch_bounds__(TILE::kThreads) void forward_kernel(const char* __restrict__ x, const char* __restrict__ w,
+__global__ __launch_bounds__(TILE::kThreads, 2) void forward_kernel(const char* __restrict__ x, const char* __restrict__ w,
                                                                  const char* __restrict__ bias,
                                                                  const int32_t* __restrict__ offsets, int64_t rows, int d_in,
                                                                  int d_out, int E, int act, char* __restrict__ pre,
@@ -300,7 +337,7 @@ __global__ __launch_bounds__(TILE::kThreads) void forward_kernel(const char* __r
 }
 
 template <typename DT, typename TILE, int BP, int BQ>
-__global__ __launch_bounds__(TILE::kThreads) void input_grad_kernel(const char* __restrict__ grad_out,
+__global__ __launch_bounds__(TILE::kThreads, 2) void input_grad_kernel(const char* __restrict__ grad_out,
                                                                     const char* __restrict__ w,
                                                                     const int32_t* __restrict__ offsets, int64_t rows,
                                                                     int d_in, int d_out, int E, int act,
@@ -330,7 +367,7 @@ __global__ __launch_bounds__(TILE::kThreads) void input_grad_kernel(const char* 
 }
 
 template <typename DT, typename TILE, int BP, int BQ>
-__global__ __launch_bounds__(TILE::kThreads) void weight_grad_kernel(const char* __restrict__ grad_out,
+__global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const char* __restrict__ grad_out,
                                                                      const char* __restrict__ x,
                                                                      const int32_t* __restrict__ offsets, int64_t rows,
                                                                      int d_in, int d_out, int E, char* __restrict__ grad_w,
