@@ -13,8 +13,10 @@
 // The matrix instruction takes P as its first operand: a lane then holds runs of 4 consecutive p of one q.
 //
 // A workgroup computes a tile of BQ x BP outputs.  k goes by chunks: 128 bytes of every row of an operand that is
-// contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into one of
-// two buffers while the waves work on the other, one barrier to a chunk.
+// contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into rings of
+// three chunks of P and two of Q (160 KB for two workgroups of binary32 or one of bf16), one barrier to a chunk.  A wave
+// starts one load per half step, between its products: a chunk's loads all at once fill the address units' queue, and the
+// products behind them wait.
 #include <type_traits>
 #include <utility>
 
@@ -109,17 +111,21 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
     }
   }
 
-  // Starts the loads of the next chunk into lds; k_bytes: what is left of a row.
-  __device__ __forceinline__ void load(uint32_t lds, int64_t k_bytes) {
-    const uint32_t dst = lds + (uint32_t)((int)threadIdx.x / 64) * 1024;
-    i32x4 buffer = buffer_of(base, bytes);
-    asm volatile("s_nop 4" : "+s"(buffer));    // the descriptor may come from vector instructions: five cycles before its use
-    const bool cut = !COLUMNS && (int64_t)k_piece >= k_bytes;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      load16_to_lds(buffer, cut ? kNowhere : offset[i], __builtin_amdgcn_readfirstlane(dst + i * WAVES * 1024));
+  i32x4 buffer;           // descriptor of the chunk being loaded
+  bool cut;               // the lane's piece is behind the end of the rows
+
+  // Prepares the loads of the next chunk; k_bytes: what is left of a row (may be nothing: the loads then bring zeros).
+  __device__ __forceinline__ void next(int64_t k_bytes) {
+    buffer = buffer_of(base, bytes);
+    // the descriptor may come from vector instructions: five cycles before its use
+    asm volatile("s_nop 4" : "+s"(buffer));
+    cut = !COLUMNS && (int64_t)k_piece >= k_bytes;
     base += chunk_step;
     bytes -= chunk_step;
+  }
+  // Starts load i of the chunk; lds: where the ring's slot has the wave's first 1024 bytes.
+  __device__ __forceinline__ void load(int i, uint32_t lds) const {
+    load16_to_lds(buffer, cut ? kNowhere : offset[i], lds + i * WAVES * 1024);
   }
 };
 
@@ -177,8 +183,10 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
   typedef Operand<DT, P_COLUMNS, BP, kWaves> OpP;
   typedef Operand<DT, Q_COLUMNS, BQ, kWaves> OpQ;
   static constexpr int kPieceReads = std::is_same<DT, BF16>::value ? 8 : 4;   // bytes that one read of columns gives a lane
-  static constexpr int kBuffer = OpP::kBytes + OpQ::kBytes;
-  static constexpr size_t kLds = 2 * (size_t)kBuffer;
+  static constexpr int kRingP = 3, kRingQ = 2;                    // chunks in LDS
+  static constexpr int kAtQ = kRingP * OpP::kBytes;
+  static constexpr size_t kLds = kAtQ + (size_t)kRingQ * OpQ::kBytes;
+  static_assert(OpP::kLoads == 4 && OpQ::kLoads == 4 && kSteps == 4 && TP % 2 == 0, "two loads of a chunk to a step");
 
   f32x16 acc[TP][TQ];
   f32x16 sums[TQ];          // Q summed over k, where wanted
@@ -188,7 +196,7 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     extern __shared__ uint4 lds[];
     lds_char* const base = (lds_char*)lds;
     const uint32_t lds_at = (uint32_t)(uintptr_t)base;
-    const int wave = (int)threadIdx.x / 64;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const Fragments<DT, P_COLUMNS, BP, TP> fp(wave % WP * TP * 32);
     const Fragments<DT, Q_COLUMNS, BQ, TQ> fq(wave / WP * TQ * 32);
 #pragma unroll
@@ -199,62 +207,92 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     }
     const uint32_t one = std::is_same<DT, BF16>::value ? 0x3f803f80u : 0x3f800000u;
     const u32x4 ones = {one, one, one, one};
-    int64_t left = K * ItemSize<DT>::value;      // bytes of k whose loads are to be started
     const int chunks = (int)((K + OpP::kChunk - 1) / OpP::kChunk);
-    auto start = [&](int slot) {
-      P.load(lds_at + slot * kBuffer, left);
-      Q.load(lds_at + slot * kBuffer + OpP::kBytes, left);
-      left -= kChunkBytes;
+    int64_t left_p = K * ItemSize<DT>::value, left_q = left_p;   // bytes of k whose loads are to be started
+    uint32_t to_p = lds_at + wave * 1024, to_q = to_p + kAtQ;    // where they go
+    int slot_p = 0;                                              // ring slot of the chunk at work
+    auto next_p = [&] {
+      P.next(left_p);
+      left_p -= kChunkBytes;
     };
+    auto next_q = [&] {
+      Q.next(left_q);
+      left_q -= kChunkBytes;
+    };
+    // Chunks 0 and 1 of Q, 0, 1 and 2 of P.  Chunks behind the last one are loaded like the others (as zeros, without a read),
+    // so that the number of loads in flight is always the same.
+#pragma unroll
+    for (int c = 0; c < kRingP; ++c) {
+      if (c < kRingQ) {
+        next_q();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Q.load(i, to_q + c * OpQ::kBytes);
+      }
+      next_p();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) P.load(i, to_p + c * OpP::kBytes);
+    }
     u32x4 a[2][TP], b[2][TQ];        // fragments of a step and of the one after it
-    auto read = [&](int into, lds_char* from, int s) {
-#pragma unroll
-      for (int t = 0; t < TP; ++t) a[into][t] = fp.read(from, s, t);
-#pragma unroll
-      for (int u = 0; u < TQ; ++u) b[into][u] = fq.read(from + OpP::kBytes, s, u);
-    };
-    if (chunks > 0) start(0);
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    asm volatile("s_waitcnt vmcnt(12)" : : : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
-    if (chunks > 1) start(1);
-    read(0, base, 0);
-    for (int c = 0; c < chunks; ++c) {
-      lds_char* const now = base + (c & 1) * kBuffer;
-      lds_char* const next = base + (~c & 1) * kBuffer;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        // the fragments of the next step are on their way while this one's products run
-        if (s + 1 < kSteps) {
-          read((s + 1) & 1, now, s + 1);
-        } else {
-          // The last fragments of chunk c are in registers, this wave's share of chunk c + 1 has landed.  Behind the barrier that
-          // is so for all waves: chunk c's buffer is free for chunk c + 2, chunk c + 1 may be read.
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+    for (int t = 0; t < TP; ++t) a[0][t] = fp.read(base, 0, t);
+#pragma unroll
+    for (int u = 0; u < TQ; ++u) b[0][u] = fq.read(base + kAtQ, 0, u);
+    for (int c = 0; c < chunks; ++c) {
+      lds_char* const now_p = base + slot_p * OpP::kBytes;
+      lds_char* const now_q = base + kAtQ + (c & 1) * OpQ::kBytes;
+      const int slot_next = slot_p == kRingP - 1 ? 0 : slot_p + 1;
+      lds_char* const next_p_at = base + slot_next * OpP::kBytes;
+      lds_char* const next_q_at = base + kAtQ + (~c & 1) * OpQ::kBytes;
+      static_for<kSteps>([&](auto sc) {
+        constexpr int s = decltype(sc)::value, now = s & 1, then = now ^ 1, sn = (s + 1) % kSteps;
+        if (s == kSteps - 1) {
+          // The last fragments of chunk c are in registers, this wave's share of chunk c + 1 has landed (P's of chunk c + 2 may be
+          // under way).  Behind the barrier that is so for all waves: chunk c's slots are free, chunk c + 1 may be read.
+          asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" : : : "memory");
           __builtin_amdgcn_s_barrier();
           asm volatile("" : : : "memory");
-          if (c + 2 < chunks) start(c & 1);
-          read(0, next, 0);
         }
+        lds_char* const from_p = s == kSteps - 1 ? next_p_at : now_p;
+        lds_char* const from_q = s == kSteps - 1 ? next_q_at : now_q;
+        static_for<2>([&](auto hc) {
+          constexpr int half = decltype(hc)::value;
+          // loads: the first two of Q's chunk c + 2 now, the other two and P's chunk c + 3 in the next chunk's steps 0 to 2
+          if (s == 3 && half == 0) next_q();
+          if (s == 3) Q.load(half, to_q + (c & 1) * OpQ::kBytes);
+          if (s == 0 && c > 0) Q.load(2 + half, to_q + (~c & 1) * OpQ::kBytes);
+          if (s == 1 && half == 0 && c > 0) next_p();
+          if ((s == 1 || s == 2) && c > 0) P.load(2 * (s - 1) + half, to_p + (slot_p == 0 ? kRingP - 1 : slot_p - 1) * OpP::kBytes);
+          __builtin_amdgcn_sched_barrier(0);
+          // the fragments of the next step are on their way while this one's products run
 #pragma unroll
-        for (int t = 0; t < TP; ++t)
+          for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t) a[then][t] = fp.read(from_p, sn, t);
 #pragma unroll
-          for (int u = 0; u < TQ; ++u) mma<DT>(a[s & 1][t], b[s & 1][u], acc[t][u]);
-        if (SUMS)
+          for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) b[then][u] = fq.read(from_q, sn, u);
 #pragma unroll
-          for (int u = 0; u < TQ; ++u) mma<DT>(ones, b[s & 1][u], sums[u]);
-        // reads and products take turns
-        constexpr int kReads = TP * (P_COLUMNS ? 16 / kPieceReads : 1) + TQ * (Q_COLUMNS ? 16 / kPieceReads : 1);
-        constexpr int kProducts = (TP * TQ + (SUMS ? TQ : 0)) * (std::is_same<DT, BF16>::value ? 1 : 4);
-        static_for<TP * TQ>([&](auto i) {
-          constexpr int n = decltype(i)::value;
-          __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / (TP * TQ) - kReads * n / (TP * TQ), 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / (TP * TQ) - kProducts * n / (TP * TQ), 0);
+          for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t)
+#pragma unroll
+            for (int u = 0; u < TQ; ++u) mma<DT>(a[now][t], b[now][u], acc[t][u]);
+          if (SUMS)
+#pragma unroll
+            for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) mma<DT>(ones, b[now][u], sums[u]);
+          // reads and products take turns
+          constexpr int kReads = TP / 2 * (P_COLUMNS ? 16 / kPieceReads : 1) + TQ / 2 * (Q_COLUMNS ? 16 / kPieceReads : 1);
+          constexpr int kTurns = TP / 2 * TQ;
+          constexpr int kProducts = (kTurns + (SUMS ? TQ / 2 : 0)) * (std::is_same<DT, BF16>::value ? 1 : 4);
+          static_for<kTurns>([&](auto i) {
+            constexpr int n = decltype(i)::value;
+            __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / kTurns - kReads * n / kTurns, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / kTurns - kProducts * n / kTurns, 0);
+          });
+          __builtin_amdgcn_sched_barrier(0);
         });
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      });
+      slot_p = slot_next;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing lands in LDS any more
   }
 
   // f(q, p, v): a piece's worth of results of q from p on, relative to the tile.  A wave's results go through LDS, binary32, 32 q
@@ -264,7 +302,8 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     constexpr int kElems = Piece<DT>::kElems, kRow = TP * 32 * 4, kLanes = TP * 32 / kElems;
     static_assert(kWaves * 32 * kRow <= (int)kLds && kRow % 256 == 0, "the waves' parts fit");
     extern __shared__ uint4 lds[];
-    const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 32, h = lane / 32;
+    const int lane = (int)threadIdx.x % 64, r = lane % 32, h = lane / 32;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     char* const part = reinterpret_cast<char*>(lds) + wave * 32 * kRow;
     __syncthreads();               // the other waves are done with the last chunk
 #pragma unroll
@@ -313,8 +352,8 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void forward_kernel(const char* 
   const int ptiles = (d_out + BP - 1) / BP;
   const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
   if (n < 0) return;
-  const RowTile rt = tiles.find(n / ptiles);
-  const int p0 = (int)(n % ptiles) * BP, np = min(BP, d_out - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
+  const RowTile rt = tiles.find(n, ptiles);
+  const int p0 = rt.column * BP, np = min(BP, d_out - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
   typename TILE::OpP P(w + ((int64_t)rt.expert * d_out + p0) * d_in * kItem, (uint32_t)d_in * kItem, np, d_in);
   typename TILE::OpQ Q(x + rt.first * d_in * kItem, (uint32_t)d_in * kItem, nq, d_in);
   TILE tile;
@@ -347,8 +386,8 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void input_grad_kernel(const cha
   const int ptiles = (d_in + BP - 1) / BP;
   const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
   if (n < 0) return;
-  const RowTile rt = tiles.find(n / ptiles);
-  const int p0 = (int)(n % ptiles) * BP, np = min(BP, d_in - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
+  const RowTile rt = tiles.find(n, ptiles);
+  const int p0 = rt.column * BP, np = min(BP, d_in - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
   typename TILE::OpP P(w + ((int64_t)rt.expert * d_out * d_in + p0) * kItem, (uint32_t)d_in * kItem, np, d_out);
   typename TILE::OpQ Q(grad_out + rt.first * d_out * kItem, (uint32_t)d_out * kItem, nq, d_out);
   TILE tile;

@@ -120,9 +120,9 @@ __global__ __launch_bounds__(256) void forward_kernel(const char* __restrict__ x
                                                       const void* bias, const int32_t* __restrict__ offsets, int64_t rows,
                                                       int d_in, int d_out, int E, int act, void* out) {
   const int ptiles = (d_out + kTile - 1) / kTile;
-  const RowTile t = RowTiles(offsets, E, rows, kTile).find((int64_t)linear_block() / ptiles);
+  const RowTile t = RowTiles(offsets, E, rows, kTile).find((int64_t)linear_block(), ptiles);
   if (t.expert < 0) return;
-  const int p0 = (int)(linear_block() % ptiles) * kTile;
+  const int p0 = t.column * kTile;
   const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 16, g = lane / 16;
   const int blocks = d_in / kBlock;
   const int64_t q = t.first + 16 * wave + r;

@@ -25,6 +25,7 @@ inline int64_t most_row_tiles(int64_t rows, int E, int tile) { return rows / til
 struct RowTile {
   int expert;           // -1: there is no such tile
   int64_t first, end;   // its first row, the end of its expert's rows
+  int column;           // its tile of columns
 };
 
 // The experts' row tiles of `tile` rows, in the order of the experts.  Every wave counts them by itself: lane e % 64 has expert
@@ -61,7 +62,12 @@ struct RowTiles {
     }
   }
 
-  __device__ __forceinline__ RowTile find(int64_t m) const {
+  // Tile n of the experts' row tiles by `columns` tiles of columns.  An expert's tiles go in bands of kBand row tiles, within a
+  // band column after column: the tiles that run at a time on an XCD are about as many rows as columns wide and share
+  // what they read.
+  __device__ __forceinline__ RowTile find(int64_t n, int columns) const {
+    constexpr int kBand = 4;
+    const int64_t m = n / columns;
     int64_t before = 0;                       // tiles of the experts below e0
     int l = lo, h = hi, u = upto;
     for (int e0 = 0;;) {
@@ -69,13 +75,15 @@ struct RowTiles {
       if (past != 0) {
         const int at = __ffsll((unsigned long long)past) - 1;
         const int rlo = __builtin_amdgcn_readlane(l, at), rhi = __builtin_amdgcn_readlane(h, at);
-        const int upto_at = __builtin_amdgcn_readlane(u, at);
-        const int64_t skipped = m - before - (upto_at - (rhi - rlo + tile - 1) / tile);
-        return {e0 + at, rlo + skipped * tile, rhi};
+        const int count_at = (rhi - rlo + tile - 1) / tile;
+        const int64_t inside = n - (before + __builtin_amdgcn_readlane(u, at) - count_at) * columns;   // its number in the expert
+        const int band = (int)(inside / ((int64_t)kBand * columns)), rest = (int)(inside - (int64_t)band * kBand * columns);
+        const int wide = min(kBand, count_at - band * kBand);
+        return {e0 + at, rlo + (int64_t)(band * kBand + rest % wide) * tile, rhi, rest / wide};
       }
       before += __builtin_amdgcn_readlane(u, kWave - 1);
       e0 += kWave;
-      if (e0 >= E) return {-1, 0, 0};
+      if (e0 >= E) return {-1, 0, 0, 0};
       count(e0, l, h, u);
     }
   }
