@@ -12,11 +12,12 @@
 //   weight       q = d_out, p = d_in, k = row       Q = grad_out contiguous in q, P = x contiguous in p
 // The matrix instruction takes P as its first operand: a lane then holds runs of 4 consecutive p of one q.
 //
-// A workgroup computes a tile of BQ x BP outputs.  k goes by chunks: 128 bytes of every row of an operand that is
-// contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into rings of
-// three chunks of P and two of Q (160 KB for two workgroups of binary32 or one of bf16), one barrier to a chunk.  A wave
-// starts one load per half step, between its products: a chunk's loads all at once fill the address units' queue, and the
-// products behind them wait.
+// A workgroup computes tiles of BQ x BP outputs, one after the other.  k goes by chunks: 128 bytes of every row of an operand
+// that is contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into
+// rings of three chunks of P and two of Q (160 KB for two workgroups of binary32 or one of bf16), one barrier to a chunk.
+// A wave starts one load per half step, between its products: a chunk's loads all at once fill the address units' queue,
+// and the products behind them wait.  The chunks of all tiles of a workgroup are one stream: while a tile's results are
+// stored, the first chunks of the next are on their way.
 #include <type_traits>
 #include <utility>
 
@@ -29,6 +30,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
@@ -79,18 +81,18 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
   static constexpr int kRowPieces = COLUMNS ? B * kItem / 16 : kPieces;   // pieces of a line of LDS
   static_assert(kLoads * 1024 * WAVES == kBytes, "whole instructions");
 
-  const char* base;       // the tile's first element, chunk 0
-  int64_t bytes;          // from there to the end of what may be read
-  int64_t chunk_step;     // bytes from one chunk to the next
-  uint32_t offset[kLoads];
-  uint32_t k_piece;       // rows: the lane's piece within the chunk, in bytes
+  uint32_t offset[kLoads];   // of the lane's pieces from the chunk's first element
+  uint32_t k_piece;          // rows: the lane's piece within the chunk, in bytes
+  uint32_t stride;           // bytes from one index (rows) or k (columns) to the next
+  // what is loaded next
+  const char* base;          // its first element
+  int64_t bytes;             // from there to the end of what may be read
+  int left;                  // rows: bytes of k from there on
+  i32x4 buffer;              // descriptor of the chunk being loaded
+  bool cut;                  // the lane's piece of it is behind the end of the rows
 
-  // element (index i, k) is at first + i * stride + k * item (rows) or first + k * stride + i * item (columns); `indices` of the
-  // tile and K of k exist; columns: a line has `line` bytes behind the tile's first index
-  __device__ __forceinline__ Operand(const char* first, uint32_t stride, int indices, int64_t K) {
+  __device__ __forceinline__ explicit Operand(uint32_t stride_) : k_piece(0), stride(stride_) {
     const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
-    base = first;
-    k_piece = 0;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int slot = (i * WAVES + wave) * 64 + lane, line = slot / kRowPieces, s = slot % kRowPieces;
@@ -102,26 +104,26 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
         offset[i] = (uint32_t)line * stride + k_piece;
       }
     }
-    if (COLUMNS) {
-      bytes = K == 0 ? 0 : (K - 1) * (int64_t)stride + indices * kItem;
-      chunk_step = (int64_t)kChunk * stride;
-    } else {
-      bytes = indices == 0 ? 0 : (int64_t)(indices - 1) * stride + K * kItem;
-      chunk_step = kChunkBytes;
-    }
   }
 
-  i32x4 buffer;           // descriptor of the chunk being loaded
-  bool cut;               // the lane's piece is behind the end of the rows
-
-  // Prepares the loads of the next chunk; k_bytes: what is left of a row (may be nothing: the loads then bring zeros).
-  __device__ __forceinline__ void next(int64_t k_bytes) {
+  // A tile's operand: element (index i, k) is at first + i * stride + k * item (rows) or first + k * stride + i * item
+  // (columns); `indices` of the tile and K of k exist.
+  __device__ __forceinline__ void start(const char* first, int indices, int K) {
+    base = first;
+    left = K * kItem;
+    bytes = COLUMNS ? (int64_t)(K - 1) * stride + indices * kItem : (int64_t)(indices - 1) * stride + K * kItem;
+    if (K == 0 || indices == 0) bytes = 0;
+  }
+  // Prepares the loads of the next chunk.  Behind the last one the loads bring zeros and read nothing.
+  __device__ __forceinline__ void next() {
     buffer = buffer_of(base, bytes);
     // the descriptor may come from vector instructions: five cycles before its use
     asm volatile("s_nop 4" : "+s"(buffer));
-    cut = !COLUMNS && (int64_t)k_piece >= k_bytes;
-    base += chunk_step;
-    bytes -= chunk_step;
+    cut = !COLUMNS && (int)k_piece >= left;
+    const int64_t step = COLUMNS ? (int64_t)kChunk * stride : kChunkBytes;
+    base += step;
+    bytes -= step;
+    left -= kChunkBytes;
   }
   // Starts load i of the chunk; lds: where the ring's slot has the wave's first 1024 bytes.
   __device__ __forceinline__ void load(int i, uint32_t lds) const {
@@ -189,267 +191,521 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
   static_assert(OpP::kLoads == 4 && OpQ::kLoads == 4 && kSteps == 4 && TP % 2 == 0, "two loads of a chunk to a step");
 
   f32x16 acc[TP][TQ];
-  f32x16 sums[TQ];          // Q summed over k, where wanted
+  float sums[TQ];           // where wanted: Q summed over the k that the lane half holds
+  u32x4 a[2][TP], b[2][TQ]; // fragments of a step and of the one after it
 
-  // K: elements of k.  SUMS: also the sums of Q over k.
-  template <bool SUMS> __device__ __forceinline__ void run(OpP& P, OpQ& Q, int64_t K) {
+  __device__ __forceinline__ static void add_elements(const u32x4& q, float& sum) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (ItemSize<DT>::value == 2) sum += __uint_as_float(q[i] << 16);
+      sum += __uint_as_float(ItemSize<DT>::value == 2 ? q[i] & 0xffff0000u : q[i]);
+    }
+  }
+
+  // One chunk's products, the loads of chunks ahead, the fragments of the next chunk's first step.  Loads in the order Q's chunk
+  // c + 2 (two behind the barrier of chunk c, two in step 0 of chunk c + 1) and P's chunk c + 3 (steps 1 and 2); at a tile's
+  // last chunk all of Q's are started before the results' stores, and its successor skips them.
+  // kBehind: vector-memory operations that a wave may have started behind the loads that the barrier stands for.
+  template <bool SUMS, typename NextP, typename NextQ>
+  __device__ __forceinline__ void chunk(const Fragments<DT, P_COLUMNS, BP, TP>& fp, const Fragments<DT, Q_COLUMNS, BQ, TQ>& fq,
+                                        OpP& P, OpQ& Q, NextP&& next_p, NextQ&& next_q, lds_char* base, uint32_t to_p,
+                                        uint32_t to_q, int& slot_p, int& slot_q, bool first, bool last, bool stores) {
+    lds_char* const now_p = base + slot_p * OpP::kBytes;
+    lds_char* const now_q = base + kAtQ + slot_q * OpQ::kBytes;
+    const int slot_next = slot_p == kRingP - 1 ? 0 : slot_p + 1, slot_free = slot_p == 0 ? kRingP - 1 : slot_p - 1;
+    lds_char* const next_p_at = base + slot_next * OpP::kBytes;
+    lds_char* const next_q_at = base + kAtQ + (slot_q ^ 1) * OpQ::kBytes;
+    static_for<kSteps>([&](auto sc) {
+      constexpr int s = decltype(sc)::value, now = s & 1, then = now ^ 1, sn = (s + 1) % kSteps;
+      if (s == kSteps - 1) {
+        // The last fragments of this chunk are in registers, this wave's share of the next one has landed (P's of the one after it and a
+        // finished tile's stores may be under way).  Behind the barrier that is so for all waves: this chunk's slots are
+        // free, the next one may be read.
+        if (stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(4 + kStores) : "memory");
+        else asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" : : : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+      }
+      lds_char* const from_p = s == kSteps - 1 ? next_p_at : now_p;
+      lds_char* const from_q = s == kSteps - 1 ? next_q_at : now_q;
+      static_for<2>([&](auto hc) {
+        constexpr int half = decltype(hc)::value;
+        if (s == 3 && half == 0) next_q();
+        if (s == 3) Q.load(half, to_q + slot_q * OpQ::kBytes);
+        if (s == 0 && !first) Q.load(2 + half, to_q + (slot_q ^ 1) * OpQ::kBytes);
+        if (s == 1 && half == 0) next_p();
+        if (s == 1 || s == 2) P.load(2 * (s - 1) + half, to_p + slot_free * OpP::kBytes);
+        __builtin_amdgcn_sched_barrier(0);
+        // the fragments of the next step are on their way while this one's products run
+#pragma unroll
+        for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t) a[then][t] = fp.read(from_p, sn, t);
+#pragma unroll
+        for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) b[then][u] = fq.read(from_q, sn, u);
+#pragma unroll
+        for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t)
+#pragma unroll
+          for (int u = 0; u < TQ; ++u) mma<DT>(a[now][t], b[now][u], acc[t][u]);
+        if (SUMS) {
+#pragma unroll
+          for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) add_elements(b[now][u], sums[u]);
+        }
+        // reads and products take turns
+        constexpr int kReads = TP / 2 * (P_COLUMNS ? 16 / kPieceReads : 1) + TQ / 2 * (Q_COLUMNS ? 16 / kPieceReads : 1);
+        constexpr int kTurns = TP / 2 * TQ;
+        constexpr int kProducts = kTurns * (std::is_same<DT, BF16>::value ? 1 : 4);
+        static_for<kTurns>([&](auto i) {
+          constexpr int n = decltype(i)::value;
+          __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / kTurns - kReads * n / kTurns, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / kTurns - kProducts * n / kTurns, 0);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+    if (last) {
+      Q.load(2, to_q + slot_q * OpQ::kBytes);
+      Q.load(3, to_q + slot_q * OpQ::kBytes);
+    }
+    slot_p = slot_next;
+    slot_q ^= 1;
+  }
+
+  // The tiles n, n + step, .. below end.  JOB: place(n) gives a tile's operands and where its results go, finish(place, tile) stores
+  // them, with kStores stores to a wave or more.
+  template <typename JOB> __device__ __forceinline__ void run(const JOB& job, int n, int end, int step) {
     extern __shared__ uint4 lds[];
+    if (n >= end) return;
     lds_char* const base = (lds_char*)lds;
-    const uint32_t lds_at = (uint32_t)(uintptr_t)base;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const uint32_t to_p = (uint32_t)(uintptr_t)base + wave * 1024, to_q = to_p + kAtQ;   // where a wave's loads go
     const Fragments<DT, P_COLUMNS, BP, TP> fp(wave % WP * TP * 32);
     const Fragments<DT, Q_COLUMNS, BQ, TQ> fq(wave / WP * TQ * 32);
-#pragma unroll
-    for (int u = 0; u < TQ; ++u) {
-#pragma unroll
-      for (int t = 0; t < TP; ++t) acc[t][u] = (f32x16){};
-      sums[u] = (f32x16){};
-    }
-    const uint32_t one = std::is_same<DT, BF16>::value ? 0x3f803f80u : 0x3f800000u;
-    const u32x4 ones = {one, one, one, one};
-    const int chunks = (int)((K + OpP::kChunk - 1) / OpP::kChunk);
-    int64_t left_p = K * ItemSize<DT>::value, left_q = left_p;   // bytes of k whose loads are to be started
-    uint32_t to_p = lds_at + wave * 1024, to_q = to_p + kAtQ;    // where they go
-    int slot_p = 0;                                              // ring slot of the chunk at work
+    OpP P(job.p_stride());
+    OpQ Q(job.q_stride());
+    typename JOB::Place here = job.place(n);
+    // the tiles that P's and Q's loads are at, and their chunks that are still to be loaded
+    int n_p = n, n_q = n, chunks_p = here.chunks(), chunks_q = chunks_p;
+    P.start(here.p, here.np, here.K);
+    Q.start(here.q, here.nq, here.K);
     auto next_p = [&] {
-      P.next(left_p);
-      left_p -= kChunkBytes;
+      if (chunks_p == 0) {
+        n_p += step;
+        const typename JOB::Place place = n_p < end ? job.place(n_p) : JOB::Place::none(here);
+        P.start(place.p, place.np, place.K);
+        chunks_p = place.chunks();
+      }
+      P.next();
+      --chunks_p;
     };
     auto next_q = [&] {
-      Q.next(left_q);
-      left_q -= kChunkBytes;
-    };
-    // Chunks 0 and 1 of Q, 0, 1 and 2 of P.  Chunks behind the last one are loaded like the others (as zeros, without a read),
-    // so that the number of loads in flight is always the same.
-#pragma unroll
-    for (int c = 0; c < kRingP; ++c) {
-      if (c < kRingQ) {
-        next_q();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) Q.load(i, to_q + c * OpQ::kBytes);
+      if (chunks_q == 0) {
+        n_q += step;
+        const typename JOB::Place place = n_q < end ? job.place(n_q) : JOB::Place::none(here);
+        Q.start(place.q, place.nq, place.K);
+        chunks_q = place.chunks();
       }
+      Q.next();
+      --chunks_q;
+    };
+    next_q();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Q.load(i, to_q);
+    for (int c = 0; c < 2; ++c) {
       next_p();
 #pragma unroll
       for (int i = 0; i < 4; ++i) P.load(i, to_p + c * OpP::kBytes);
     }
-    u32x4 a[2][TP], b[2][TQ];        // fragments of a step and of the one after it
-    asm volatile("s_waitcnt vmcnt(12)" : : : "memory");
+    asm volatile("s_waitcnt vmcnt(4)" : : : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
+    next_q();
 #pragma unroll
-    for (int t = 0; t < TP; ++t) a[0][t] = fp.read(base, 0, t);
+    for (int i = 0; i < 4; ++i) Q.load(i, to_q + OpQ::kBytes);
+    int slot_p = 0, slot_q = 0;
+    bool stores = false;
+    for (;;) {
+      // the first fragments (again behind a finished tile: they would take registers that its results need)
 #pragma unroll
-    for (int u = 0; u < TQ; ++u) b[0][u] = fq.read(base + kAtQ, 0, u);
-    for (int c = 0; c < chunks; ++c) {
-      lds_char* const now_p = base + slot_p * OpP::kBytes;
-      lds_char* const now_q = base + kAtQ + (c & 1) * OpQ::kBytes;
-      const int slot_next = slot_p == kRingP - 1 ? 0 : slot_p + 1;
-      lds_char* const next_p_at = base + slot_next * OpP::kBytes;
-      lds_char* const next_q_at = base + kAtQ + (~c & 1) * OpQ::kBytes;
-      static_for<kSteps>([&](auto sc) {
-        constexpr int s = decltype(sc)::value, now = s & 1, then = now ^ 1, sn = (s + 1) % kSteps;
-        if (s == kSteps - 1) {
-          // The last fragments of chunk c are in registers, this wave's share of chunk c + 1 has landed (P's of chunk c + 2 may be
-          // under way).  Behind the barrier that is so for all waves: chunk c's slots are free, chunk c + 1 may be read.
-          asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" : : : "memory");
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" : : : "memory");
-        }
-        lds_char* const from_p = s == kSteps - 1 ? next_p_at : now_p;
-        lds_char* const from_q = s == kSteps - 1 ? next_q_at : now_q;
-        static_for<2>([&](auto hc) {
-          constexpr int half = decltype(hc)::value;
-          // loads: the first two of Q's chunk c + 2 now, the other two and P's chunk c + 3 in the next chunk's steps 0 to 2
-          if (s == 3 && half == 0) next_q();
-          if (s == 3) Q.load(half, to_q + (c & 1) * OpQ::kBytes);
-          if (s == 0 && c > 0) Q.load(2 + half, to_q + (~c & 1) * OpQ::kBytes);
-          if (s == 1 && half == 0 && c > 0) next_p();
-          if ((s == 1 || s == 2) && c > 0) P.load(2 * (s - 1) + half, to_p + (slot_p == 0 ? kRingP - 1 : slot_p - 1) * OpP::kBytes);
-          __builtin_amdgcn_sched_barrier(0);
-          // the fragments of the next step are on their way while this one's products run
+      for (int t = 0; t < TP; ++t) a[0][t] = fp.read(base + slot_p * OpP::kBytes, 0, t);
 #pragma unroll
-          for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t) a[then][t] = fp.read(from_p, sn, t);
+      for (int u = 0; u < TQ; ++u) b[0][u] = fq.read(base + kAtQ + slot_q * OpQ::kBytes, 0, u);
 #pragma unroll
-          for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) b[then][u] = fq.read(from_q, sn, u);
+      for (int u = 0; u < TQ; ++u) {
 #pragma unroll
-          for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t)
-#pragma unroll
-            for (int u = 0; u < TQ; ++u) mma<DT>(a[now][t], b[now][u], acc[t][u]);
-          if (SUMS)
-#pragma unroll
-            for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) mma<DT>(ones, b[now][u], sums[u]);
-          // reads and products take turns
-          constexpr int kReads = TP / 2 * (P_COLUMNS ? 16 / kPieceReads : 1) + TQ / 2 * (Q_COLUMNS ? 16 / kPieceReads : 1);
-          constexpr int kTurns = TP / 2 * TQ;
-          constexpr int kProducts = (kTurns + (SUMS ? TQ / 2 : 0)) * (std::is_same<DT, BF16>::value ? 1 : 4);
-          static_for<kTurns>([&](auto i) {
-            constexpr int n = decltype(i)::value;
-            __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / kTurns - kReads * n / kTurns, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / kTurns - kProducts * n / kTurns, 0);
-          });
-          __builtin_amdgcn_sched_barrier(0);
-        });
-      });
-      slot_p = slot_next;
+        for (int t = 0; t < TP; ++t) acc[t][u] = (f32x16){};
+        sums[u] = 0.0f;
+      }
+      const int chunks = here.chunks();
+      if (JOB::kSums && job.sums(here)) {
+        for (int c = 0; c < chunks; ++c)
+          chunk<JOB::kSums>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, c == 0, c == chunks - 1, stores && c == 0);
+      } else {
+        for (int c = 0; c < chunks; ++c)
+          chunk<false>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, c == 0, c == chunks - 1, stores && c == 0);
+      }
+      job.finish(here, *this);
+      stores = true;
+      n += step;
+      if (n >= end) break;
+      here = job.place(n);
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing lands in LDS any more
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // nothing is on its way to LDS when the workgroup ends
   }
 
-  // f(q, p, v): a piece's worth of results of q from p on, relative to the tile.  A wave's results go through LDS, binary32, 32 q
-  // at a time, so that the 16 bytes that a lane reads and writes of the outputs are next to its neighbours': 256 bytes
-  // of an output row at a time instead of 16.  Slots of 16 bytes are moved by the row against bank conflicts.
-  template <typename F> __device__ __forceinline__ void finish(F&& f) const {
-    constexpr int kElems = Piece<DT>::kElems, kRow = TP * 32 * 4, kLanes = TP * 32 / kElems;
-    static_assert(kWaves * 32 * kRow <= (int)kLds && kRow % 256 == 0, "the waves' parts fit");
-    extern __shared__ uint4 lds[];
-    const int lane = (int)threadIdx.x % 64, r = lane % 32, h = lane / 32;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-    char* const part = reinterpret_cast<char*>(lds) + wave * 32 * kRow;
-    __syncthreads();               // the other waves are done with the last chunk
-#pragma unroll
-    for (int u = 0; u < TQ; ++u) {
-#pragma unroll
-      for (int t = 0; t < TP; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *reinterpret_cast<float4*>(part + r * kRow + ((8 * t + 2 * j + h) ^ (r & 15)) * 16) =
-              make_float4(acc[t][u][4 * j], acc[t][u][4 * j + 1], acc[t][u][4 * j + 2], acc[t][u][4 * j + 3]);
-      __builtin_amdgcn_wave_barrier();
-      asm volatile("" : : : "memory");
-#pragma unroll
-      for (int i = 0; i < 32 * kLanes / 64; ++i) {
-        const int q = i * (64 / kLanes) + lane / kLanes, c = lane % kLanes;
-        float v[kElems];
-#pragma unroll
-        for (int j = 0; j < kElems / 4; ++j) {
-          const float4 w = *reinterpret_cast<const float4*>(part + q * kRow + ((c * (kElems / 4) + j) ^ (q & 15)) * 16);
-          v[4 * j] = w.x; v[4 * j + 1] = w.y; v[4 * j + 2] = w.z; v[4 * j + 3] = w.w;
-        }
-        f((wave / WP * TQ + u) * 32 + q, wave % WP * TP * 32 + c * kElems, v);
+  // ---- results: lanes and memory.  Of the 32 x 32 results of tiles t, u a lane has q = r = lane % 32 and, h = lane / 32, p = 8 j + 4 h
+  // + 0 .. 3 for j = 0 .. 3.  Two exchanges between lanes make that 16 bytes of consecutive p to a lane, 64 bytes of 16 rows to
+  // an instruction: lane l then has q = 16 i + l % 16 and the piece number piece(l), i = 0, 1 (bf16; four of 16 bytes in
+  // binary32: two times 16 q by two times 64 bytes).
+  static constexpr int kSlots = ItemSize<DT>::value;        // 16-byte pieces of a lane per 32 x 32 results
+  static constexpr int kStores = TP * TQ * kSlots;
+
+  struct Lines {
+    __amdgpu_buffer_rsrc_t buffer;
+    uint32_t at, ld;     // the lane's first piece of the wave's part; bytes of a line
+    int p, np;           // its column; columns that exist
+  };
+  // first: the tile's first element in an array of lines of ld bytes; nq by np of it exist.
+  __device__ __forceinline__ static Lines lines(const char* first, uint32_t ld, int nq, int np) {
+    const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int64_t bytes = nq == 0 ? 0 : (int64_t)(nq - 1) * ld + np * ItemSize<DT>::value;
+    Lines l;
+    l.buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
+    l.ld = ld;
+    l.p = wave % WP * TP * 32 + (ItemSize<DT>::value == 2 ? 16 * (lane / 16 % 2) + 8 * (lane / 32) : 8 * (lane / 16 % 2) + 4 * (lane / 32));
+    l.np = np;
+    l.at = (uint32_t)(wave / WP * TQ * 32 + lane % 16) * ld + (uint32_t)l.p * ItemSize<DT>::value;
+    return l;
+  }
+  // Offset of the lane's piece i of tiles t, u; behind the end of the buffer where there is no such column (or line).
+  __device__ __forceinline__ static uint32_t piece_at(const Lines& l, int t, int u, int i) {
+    const int column = 32 * t + (ItemSize<DT>::value == 2 ? 0 : i / 2 * 16), line = 32 * u + i % 2 * 16;
+    return l.p + column < l.np ? l.at + (uint32_t)line * l.ld + (uint32_t)column * ItemSize<DT>::value : kNowhere;
+  }
+  __device__ __forceinline__ static void swap32(uint32_t& x, uint32_t& y) {
+    const auto v = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    x = v[0];
+    y = v[1];
+  }
+  __device__ __forceinline__ static void swap16(uint32_t& x, uint32_t& y) {
+    const auto v = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = v[0];
+    y = v[1];
+  }
+  // The exchanges, their own inverse.  bf16: w[2 j + i] is the pair of p 8 j + 4 h + 2 i; piece i afterwards w[4 i .. 4 i + 3].
+  // binary32: w[4 j + i] is p 8 j + 4 h + i; piece i afterwards w[4 i .. 4 i + 3].
+  __device__ __forceinline__ static void exchange(uint32_t (&w)[4 * kSlots], bool back) {
+    if constexpr (ItemSize<DT>::value == 2) {
+      // w[0..3]: j = 0, 1; the pieces want {w0 w1 | w2 w3} with the halves joined
+      if (!back) {
+        swap32(w[0], w[2]);
+        swap32(w[1], w[3]);
+        swap32(w[4], w[6]);
+        swap32(w[5], w[7]);
       }
-      __builtin_amdgcn_wave_barrier();
-      asm volatile("" : : : "memory");
+#pragma unroll
+      for (int i = 0; i < 4; ++i) swap16(w[i], w[4 + i]);
+      if (back) {
+        swap32(w[0], w[2]);
+        swap32(w[1], w[3]);
+        swap32(w[4], w[6]);
+        swap32(w[5], w[7]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; j += 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) swap16(w[4 * j + i], w[4 * j + 4 + i]);
+    }
+  }
+  __device__ __forceinline__ static void put(const Lines& l, int t, int u, const float (&v)[16]) {
+    uint32_t w[4 * kSlots];
+    if constexpr (ItemSize<DT>::value == 2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = f32_to_bf16_pair(v[2 * i], v[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
+    }
+    exchange(w, false);
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i)
+      __builtin_amdgcn_raw_buffer_store_b128((u32x4){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]}, l.buffer,
+                                             (int)piece_at(l, t, u, i), 0, 0);
+  }
+  struct Pieces { u32x4 v[kSlots]; };
+  __device__ __forceinline__ static Pieces get(const Lines& l, int t, int u) {
+    Pieces x;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.buffer, (int)piece_at(l, t, u, i), 0, 0));
+    return x;
+  }
+  __device__ __forceinline__ static void spread(const Pieces& x, float (&v)[16]) {
+    uint32_t w[4 * kSlots];
+#pragma unroll
+    for (int i = 0; i < 4 * kSlots; ++i) w[i] = x.v[i / 4][i % 4];
+    exchange(w, true);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (ItemSize<DT>::value == 2) v[i] = __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+      else v[i] = __uint_as_float(w[i]);
+    }
+  }
+  // Four elements for each j of tile t from a line (bias); behind its end zeros.
+  __device__ __forceinline__ static void get_line(const char* line, int np, int t, float (&v)[16]) {
+    const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)line, 0, np * ItemSize<DT>::value, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = (wave % WP * TP * 32 + 32 * t + 8 * j + 4 * (lane / 32)) * ItemSize<DT>::value;
+      if constexpr (ItemSize<DT>::value == 2) {
+        const u32x2 q = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buffer, at, 0, 0));
+        v[4 * j] = __uint_as_float(q[0] << 16); v[4 * j + 1] = __uint_as_float(q[0] & 0xffff0000u);
+        v[4 * j + 2] = __uint_as_float(q[1] << 16); v[4 * j + 3] = __uint_as_float(q[1] & 0xffff0000u);
+      } else {
+        const u32x4 q = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, at, 0, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * j + i] = __uint_as_float(q[i]);
+      }
     }
   }
 };
 
-// Tile number of a workgroup out of `total`: workgroups go round the 8 XCDs, each XCD gets consecutive tiles, so that what
-// neighbouring tiles share is fetched into one L2.  -1: there is none left for it.
-__device__ __forceinline__ int64_t tile_of_block(uint64_t block, int64_t total) {
-  const int64_t per = (total + 7) / 8, slot = (int64_t)(block / 8), n = (int64_t)(block % 8) * per + slot;
-  return slot < per && n < total ? n : -1;
+// Tiles of a workgroup out of `total`: workgroups go round the 8 XCDs, each XCD has a run of consecutive tiles, dealt to its
+// workgroups one by one, so that what neighbouring tiles share is fetched into one L2.
+struct Share { int first, end, step; };
+__device__ __forceinline__ Share share_of_block(int total) {
+  const int xcd = (int)(blockIdx.x % 8), mine = (int)(blockIdx.x / 8), blocks = (int)(gridDim.x / 8);
+  const int per = total / 8, more = total % 8;                // the first `more` XCDs have one tile more
+  const int first = xcd * per + min(xcd, more);
+  return {first + mine, first + per + (xcd < more ? 1 : 0), blocks};
 }
-inline uint64_t blocks_for(uint64_t tiles) { return (tiles + 7) / 8 * 8; }
+
+// A tile as Tile::run takes it.
+struct PlaceOfRows {
+  const char *p, *q;
+  int np, nq, K, chunk, expert, first, p0;
+  __device__ __forceinline__ int chunks() const { return max((K + chunk - 1) / chunk, 1); }
+  __device__ __forceinline__ static PlaceOfRows none(const PlaceOfRows& like) {
+    PlaceOfRows x = like;
+    x.np = x.nq = x.K = 0;
+    return x;
+  }
+};
+
+template <typename DT, typename TILE, int BP, int BQ> struct ForwardJob {
+  typedef PlaceOfRows Place;
+  static constexpr bool kSums = false;
+  static constexpr int kItem = ItemSize<DT>::value;
+  const char *x, *w, *bias;
+  char *pre, *out;
+  int d_in, d_out, act, ptiles;
+  const RowTiles& tiles;
+
+  __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
+  __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_in * kItem; }
+  __device__ __forceinline__ Place place(int n) const {
+    const RowTile t = tiles.find(n, ptiles);
+    const int p0 = t.column * BP;
+    return {w + ((int64_t)t.expert * d_out + p0) * d_in * kItem, x + (int64_t)t.first * d_in * kItem, min(BP, d_out - p0), t.rows,
+            d_in, TILE::OpP::kChunk, t.expert, t.first, p0};
+  }
+  __device__ __forceinline__ bool sums(const Place&) const { return false; }
+  template <int ACT, bool KEEP> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
+    const int64_t first = ((int64_t)at.first * d_out + at.p0) * kItem;
+    const typename TILE::Lines o = TILE::lines(out + first, (uint32_t)d_out * kItem, at.nq, at.np);
+    const typename TILE::Lines k = TILE::lines((KEEP ? pre : out) + first, (uint32_t)d_out * kItem, at.nq, at.np);
+#pragma unroll
+    for (int t = 0; t < TILE::TP; ++t) {
+      float b[16] = {};
+      if (bias) TILE::get_line(bias + ((int64_t)at.expert * d_out + at.p0) * kItem, at.np, t, b);
+#pragma unroll
+      for (int u = 0; u < TILE::TQ; ++u) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i] + b[i];
+        if (KEEP) TILE::put(k, t, u, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = activate(v[i], ACT);
+        TILE::put(o, t, u, v);
+      }
+    }
+  }
+  template <int ACT> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
+    if (pre) store<ACT, true>(at, tile);
+    else store<ACT, false>(at, tile);
+  }
+  __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
+    if (act == LSHMOE_ACT_RELU) store<LSHMOE_ACT_RELU>(at, tile);
+    else if (act == LSHMOE_ACT_GELU) store<LSHMOE_ACT_GELU>(at, tile);
+    else store<LSHMOE_ACT_NONE>(at, tile);
+  }
+};
 
 template <typename DT, typename TILE, int BP, int BQ>
 __global__ __launch_bounds__(TILE::kThreads, 2) void forward_kernel(const char* __restrict__ x, const char* __restrict__ w,
-                                                                 const char* __restrict__ bias,
-                                                                 const int32_t* __restrict__ offsets, int64_t rows, int d_in,
-                                                                 int d_out, int E, int act, char* __restrict__ pre,
-                                                                 char* __restrict__ out) {
-  constexpr int kItem = ItemSize<DT>::value, kElems = Piece<DT>::kElems;
+                                                                    const char* __restrict__ bias,
+                                                                    const int32_t* __restrict__ offsets, int rows, int d_in,
+                                                                    int d_out, int E, int act, char* __restrict__ pre,
+                                                                    char* __restrict__ out) {
   const RowTiles tiles(offsets, E, rows, BQ);
   const int ptiles = (d_out + BP - 1) / BP;
-  const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
-  if (n < 0) return;
-  const RowTile rt = tiles.find(n, ptiles);
-  const int p0 = rt.column * BP, np = min(BP, d_out - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
-  typename TILE::OpP P(w + ((int64_t)rt.expert * d_out + p0) * d_in * kItem, (uint32_t)d_in * kItem, np, d_in);
-  typename TILE::OpQ Q(x + rt.first * d_in * kItem, (uint32_t)d_in * kItem, nq, d_in);
+  const ForwardJob<DT, TILE, BP, BQ> job = {x, w, bias, pre, out, d_in, d_out, act, ptiles, tiles};
+  const Share s = share_of_block(tiles.total * ptiles);
   TILE tile;
-  tile.template run<false>(P, Q, d_in);
-  tile.finish([&](int q, int p, float (&v)[kElems]) {
-    if (q >= nq || p >= np) return;
-    if (bias) {
-      float b[kElems];
-      Piece<DT>::widen(load16(bias + ((int64_t)rt.expert * d_out + p0 + p) * kItem), b);
-#pragma unroll
-      for (int i = 0; i < kElems; ++i) v[i] += b[i];
-    }
-    const int64_t at = ((rt.first + q) * d_out + p0 + p) * kItem;
-    if (pre) store16(pre + at, Piece<DT>::narrow(v));
-    if (act != LSHMOE_ACT_NONE)
-#pragma unroll
-      for (int i = 0; i < kElems; ++i) v[i] = activate(v[i], act);
-    store16(out + at, Piece<DT>::narrow(v));
-  });
+  tile.run(job, s.first, s.end, s.step);
 }
+
+template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
+  typedef PlaceOfRows Place;
+  static constexpr bool kSums = false;
+  static constexpr int kItem = ItemSize<DT>::value;
+  const char *grad_out, *w, *pre;
+  char* grad_x;
+  int d_in, d_out, act, ptiles;
+  const RowTiles& tiles;
+
+  __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
+  __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_out * kItem; }
+  __device__ __forceinline__ Place place(int n) const {
+    const RowTile t = tiles.find(n, ptiles);
+    const int p0 = t.column * BP;
+    return {w + ((int64_t)t.expert * d_out * d_in + p0) * kItem, grad_out + (int64_t)t.first * d_out * kItem, min(BP, d_in - p0),
+            t.rows, d_out, TILE::OpP::kChunk, t.expert, t.first, p0};
+  }
+  __device__ __forceinline__ bool sums(const Place&) const { return false; }
+  template <int ACT> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
+    const int64_t first = ((int64_t)at.first * d_in + at.p0) * kItem;
+    const typename TILE::Lines o = TILE::lines(grad_x + first, (uint32_t)d_in * kItem, at.nq, at.np);
+    const typename TILE::Lines k = TILE::lines((ACT == LSHMOE_ACT_NONE ? grad_x : pre) + first, (uint32_t)d_in * kItem, at.nq, at.np);
+    // the values before the activation, a column tile ahead: a load waits for the stores in front of it
+    typename TILE::Pieces x[2][TILE::TQ];
+    auto get = [&](int t) {
+#pragma unroll
+      for (int u = 0; u < TILE::TQ; ++u) x[t & 1][u] = TILE::get(k, t, u);
+    };
+    if (ACT != LSHMOE_ACT_NONE) get(0);
+#pragma unroll
+    for (int t = 0; t < TILE::TP; ++t) {
+      if (ACT != LSHMOE_ACT_NONE && t + 1 < TILE::TP) get(t + 1);
+#pragma unroll
+      for (int u = 0; u < TILE::TQ; ++u) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i];
+        if (ACT != LSHMOE_ACT_NONE) {
+          float z[16];
+          TILE::spread(x[t & 1][u], z);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] *= activation_slope(z[i], ACT);
+        }
+        TILE::put(o, t, u, v);
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
+    if (act == LSHMOE_ACT_RELU) store<LSHMOE_ACT_RELU>(at, tile);
+    else if (act == LSHMOE_ACT_GELU) store<LSHMOE_ACT_GELU>(at, tile);
+    else store<LSHMOE_ACT_NONE>(at, tile);
+  }
+};
 
 template <typename DT, typename TILE, int BP, int BQ>
 __global__ __launch_bounds__(TILE::kThreads, 2) void input_grad_kernel(const char* __restrict__ grad_out,
-                                                                    const char* __restrict__ w,
-                                                                    const int32_t* __restrict__ offsets, int64_t rows,
-                                                                    int d_in, int d_out, int E, int act,
-                                                                    const char* __restrict__ pre, char* __restrict__ grad_x) {
-  constexpr int kItem = ItemSize<DT>::value, kElems = Piece<DT>::kElems;
+                                                                       const char* __restrict__ w,
+                                                                       const int32_t* __restrict__ offsets, int rows, int d_in,
+                                                                       int d_out, int E, int act,
+                                                                       const char* __restrict__ pre, char* __restrict__ grad_x) {
   const RowTiles tiles(offsets, E, rows, BQ);
   const int ptiles = (d_in + BP - 1) / BP;
-  const int64_t n = tile_of_block(linear_block(), tiles.total * ptiles);
-  if (n < 0) return;
-  const RowTile rt = tiles.find(n, ptiles);
-  const int p0 = rt.column * BP, np = min(BP, d_in - p0), nq = (int)min((int64_t)BQ, rt.end - rt.first);
-  typename TILE::OpP P(w + ((int64_t)rt.expert * d_out * d_in + p0) * kItem, (uint32_t)d_in * kItem, np, d_out);
-  typename TILE::OpQ Q(grad_out + rt.first * d_out * kItem, (uint32_t)d_out * kItem, nq, d_out);
+  const InputGradJob<DT, TILE, BP, BQ> job = {grad_out, w, pre, grad_x, d_in, d_out, act, ptiles, tiles};
+  const Share s = share_of_block(tiles.total * ptiles);
   TILE tile;
-  tile.template run<false>(P, Q, d_out);
-  tile.finish([&](int q, int p, float (&v)[kElems]) {
-    if (q >= nq || p >= np) return;
-    const int64_t at = ((rt.first + q) * d_in + p0 + p) * kItem;
-    if (act != LSHMOE_ACT_NONE) {
-      float b[kElems];
-      Piece<DT>::widen(load16(pre + at), b);
-#pragma unroll
-      for (int i = 0; i < kElems; ++i) v[i] *= activation_slope(b[i], act);
-    }
-    store16(grad_x + at, Piece<DT>::narrow(v));
-  });
+  tile.run(job, s.first, s.end, s.step);
 }
+
+template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
+  struct Place {
+    const char *p, *q;
+    int np, nq, K, expert, p0, q0;
+    __device__ __forceinline__ int chunks() const { return max((K + TILE::OpP::kChunk - 1) / TILE::OpP::kChunk, 1); }
+    __device__ __forceinline__ static Place none(const Place& like) {
+      Place x = like;
+      x.np = x.nq = x.K = 0;
+      return x;
+    }
+  };
+  static constexpr bool kSums = true;
+  static constexpr int kItem = ItemSize<DT>::value;
+  const char *grad_out, *x;
+  char *grad_w, *grad_bias;
+  int d_in, d_out, ptiles, qtiles;
+  const RowTiles& tiles;
+
+  __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
+  __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_out * kItem; }
+  __device__ __forceinline__ Place place(int n) const {
+    const int e = (int)((uint32_t)n / (uint32_t)(ptiles * qtiles)), inside = n - e * ptiles * qtiles;
+    const int q = (int)((uint32_t)inside / (uint32_t)ptiles), p0 = (inside - q * ptiles) * BP, q0 = q * BQ;
+    const RowRange range = tiles.range(e);
+    return {x + ((int64_t)range.lo * d_in + p0) * kItem, grad_out + ((int64_t)range.lo * d_out + q0) * kItem, min(BP, d_in - p0),
+            min(BQ, d_out - q0), range.hi - range.lo, e, p0, q0};
+  }
+  __device__ __forceinline__ bool sums(const Place& at) const { return grad_bias != nullptr && at.p0 == 0; }
+  __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
+    const typename TILE::Lines o = TILE::lines(grad_w + (((int64_t)at.expert * d_out + at.q0) * d_in + at.p0) * kItem,
+                                               (uint32_t)d_in * kItem, at.nq, at.np);
+#pragma unroll
+    for (int t = 0; t < TILE::TP; ++t)
+#pragma unroll
+      for (int u = 0; u < TILE::TQ; ++u) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i];
+        TILE::put(o, t, u, v);
+      }
+    if (!sums(at)) return;
+    // the waves of one column of waves have the same Q: the first stores, the lane halves' sums joined
+    constexpr int kWP = BP / 32 / TILE::TP;
+    const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
+#pragma unroll
+    for (int u = 0; u < TILE::TQ; ++u) {
+      const float sum = tile.sums[u] + __shfl_xor(tile.sums[u], 32, 64);
+      const int q = (wave / kWP * TILE::TQ + u) * 32 + lane;
+      if (wave % kWP != 0 || lane >= 32 || q >= at.nq) continue;
+      const int64_t i = (int64_t)at.expert * d_out + at.q0 + q;
+      if (kItem == 4) reinterpret_cast<float*>(grad_bias)[i] = sum;
+      else reinterpret_cast<__bf16*>(grad_bias)[i] = (__bf16)sum;
+    }
+  }
+};
 
 template <typename DT, typename TILE, int BP, int BQ>
 __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const char* __restrict__ grad_out,
-                                                                     const char* __restrict__ x,
-                                                                     const int32_t* __restrict__ offsets, int64_t rows,
-                                                                     int d_in, int d_out, int E, char* __restrict__ grad_w,
-                                                                     char* __restrict__ grad_bias) {
-  constexpr int kItem = ItemSize<DT>::value;
+                                                                        const char* __restrict__ x,
+                                                                        const int32_t* __restrict__ offsets, int rows, int d_in,
+                                                                        int d_out, int E, char* __restrict__ grad_w,
+                                                                        char* __restrict__ grad_bias) {
+  const RowTiles tiles(offsets, E, rows, BQ);
   const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ;
-  const int64_t n = tile_of_block(linear_block(), (int64_t)E * ptiles * qtiles);
-  if (n < 0) return;
-  const int64_t e = n / ((int64_t)ptiles * qtiles);
-  const int p0 = (int)(n % ptiles) * BP, q0 = (int)(n / ptiles % qtiles) * BQ;
-  const int np = min(BP, d_in - p0), nq = min(BQ, d_out - q0);
-  const RowRange range = rows_of(offsets, (int)e, rows);
-  const int64_t K = range.hi - range.lo;
-  typename TILE::OpP P(x + (range.lo * d_in + p0) * kItem, (uint32_t)d_in * kItem, np, K);
-  typename TILE::OpQ Q(grad_out + (range.lo * d_out + q0) * kItem, (uint32_t)d_out * kItem, nq, K);
+  const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, d_in, d_out, ptiles, qtiles, tiles};
+  const Share s = share_of_block(E * ptiles * qtiles);
   TILE tile;
-  const bool sums = grad_bias != nullptr && p0 == 0;
-  if (sums)
-    tile.template run<true>(P, Q, K);
-  else
-    tile.template run<false>(P, Q, K);
-  tile.finish([&](int q, int p, float (&v)[Piece<DT>::kElems]) {
-    if (q < nq && p < np) store16(grad_w + ((e * d_out + q0 + q) * d_in + p0 + p) * kItem, Piece<DT>::narrow(v));
-  });
-  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
-  if (sums && wave % (BP / 32 / TILE::TP) == 0 && lane < 32) {
-#pragma unroll
-    for (int u = 0; u < TILE::TQ; ++u) {
-      const int q = (wave / (BP / 32 / TILE::TP) * TILE::TQ + u) * 32 + lane;
-      if (q >= nq) continue;
-      const float v = tile.sums[u][0];
-      if (kItem == 4) reinterpret_cast<float*>(grad_bias)[e * d_out + q0 + q] = v;
-      else reinterpret_cast<__bf16*>(grad_bias)[e * d_out + q0 + q] = (__bf16)v;
-    }
-  }
+  tile.run(job, s.first, s.end, s.step);
 }
 
-template <typename DT> struct Shape { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4; };
-template <> struct Shape<F32> { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2; };
+template <typename DT> struct Shape { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, kPerUnit = 1; };
+template <> struct Shape<F32> { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, kPerUnit = 2; };
 
 // More than 64 KB of LDS has to be asked for, once per kernel and device; asking again is harmless.
 template <typename K> hipError_t allow_lds(K kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+constexpr int kUnits = 256;   // compute units
+
+// Workgroups for at most this many tiles: as many as run at a time, a multiple of the 8 XCDs.
+inline uint32_t blocks_for(uint64_t tiles, int per_unit) {
+  const uint64_t most = (uint64_t)kUnits * per_unit, want = (tiles + 7) / 8 * 8;
+  return (uint32_t)(want < most ? want : most);
 }
 
 template <typename DT>
@@ -460,8 +716,8 @@ hipError_t forward(const void* x, const void* w, const void* bias, const int32_t
   auto kernel = forward_kernel<DT, TILE, S::BP, S::BQ>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
   const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, S::BQ) * ((d_out + S::BP - 1) / S::BP);
-  kernel<<<grid_of_blocks(blocks_for(tiles)), TILE::kThreads, TILE::kLds, stream>>>(
-      (const char*)x, (const char*)w, (const char*)bias, offsets, rows, d_in, d_out, E, act, (char*)pre, (char*)out);
+  kernel<<<blocks_for(tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)x, (const char*)w, (const char*)bias, offsets, (int)rows, d_in, d_out, E, act, (char*)pre, (char*)out);
   return hipGetLastError();
 }
 
@@ -473,8 +729,8 @@ hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offset
   auto kernel = input_grad_kernel<DT, TILE, S::BP, S::BQ>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
   const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, S::BQ) * ((d_in + S::BP - 1) / S::BP);
-  kernel<<<grid_of_blocks(blocks_for(tiles)), TILE::kThreads, TILE::kLds, stream>>>(
-      (const char*)grad_out, (const char*)w, offsets, rows, d_in, d_out, E, act, (const char*)pre, (char*)grad_x);
+  kernel<<<blocks_for(tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)grad_out, (const char*)w, offsets, (int)rows, d_in, d_out, E, act, (const char*)pre, (char*)grad_x);
   return hipGetLastError();
 }
 
@@ -486,8 +742,8 @@ hipError_t weight_grad(const void* grad_out, const void* x, const int32_t* offse
   auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
   const uint64_t tiles = (uint64_t)E * ((d_in + S::BP - 1) / S::BP) * ((d_out + S::BQ - 1) / S::BQ);
-  kernel<<<grid_of_blocks(blocks_for(tiles)), TILE::kThreads, TILE::kLds, stream>>>(
-      (const char*)grad_out, (const char*)x, offsets, rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias);
+  kernel<<<blocks_for(tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)grad_out, (const char*)x, offsets, (int)rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias);
   return hipGetLastError();
 }
 

@@ -120,24 +120,25 @@ __global__ __launch_bounds__(256) void forward_kernel(const char* __restrict__ x
                                                       const void* bias, const int32_t* __restrict__ offsets, int64_t rows,
                                                       int d_in, int d_out, int E, int act, void* out) {
   const int ptiles = (d_out + kTile - 1) / kTile;
-  const RowTile t = RowTiles(offsets, E, rows, kTile).find((int64_t)linear_block(), ptiles);
-  if (t.expert < 0) return;
+  const RowTiles tiles(offsets, E, (int)rows, kTile);
+  if (linear_block() >= (uint64_t)tiles.total * ptiles) return;
+  const RowTile t = tiles.find((int)linear_block(), ptiles);
   const int p0 = t.column * kTile;
   const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 16, g = lane / 16;
   const int blocks = d_in / kBlock;
-  const int64_t q = t.first + 16 * wave + r;
+  const int64_t q = (int64_t)t.first + 16 * wave + r, end = (int64_t)t.first + t.rows;
   f32x4 acc[4] = {};
   for (int k = 0; k < blocks; k += 4) {
     i32x8 b, a;
     int sb, sa;
-    load_block(x_codes, x_scales, min(q, t.end - 1), blocks, k + g, b, sb);
+    load_block(x_codes, x_scales, min(q, end - 1), blocks, k + g, b, sb);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       load_block(w_codes, w_scales, (int64_t)t.expert * d_out + min(p0 + 16 * i + r, d_out - 1), blocks, k + g, a, sa);
       acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[i], 4, 4, 0, sa, 0, sb);
     }
   }
-  if (q >= t.end) return;
+  if (q >= end) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
