@@ -179,6 +179,8 @@ template <typename DT, bool COLUMNS, int B, int T> struct Fragments {
   }
 };
 
+struct TileEntry { int v[4]; };
+
 template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, int WQ> struct Tile {
   static constexpr int kWaves = WP * WQ, kThreads = 64 * kWaves;
   static constexpr int TP = BP / WP / 32, TQ = BQ / WQ / 32;     // 32 x 32 tiles of a wave
@@ -269,8 +271,10 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     slot_q ^= 1;
   }
 
-  // The tiles n, n + step, .. below end.  JOB: place(n) gives a tile's operands and where its results go, finish(place, tile) stores
-  // them, with kStores stores to a wave or more.
+  // The tiles n, n + step, .. below end.  JOB: entry(n) says which tile n is, each lane of another one; place(entry) gives a
+  // tile's operands and where its results go; finish(place, tile) stores them, with kStores stores to a wave or more.
+  // Lane i of a wave has the entry of the tile i steps on: looked up one by one, between the products, they cost
+  // 7 of a tile's 40 us at K = 1024.
   template <typename JOB> __device__ __forceinline__ void run(const JOB& job, int n, int end, int step) {
     extern __shared__ uint4 lds[];
     if (n >= end) return;
@@ -281,27 +285,38 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     const Fragments<DT, Q_COLUMNS, BQ, TQ> fq(wave / WP * TQ * 32);
     OpP P(job.p_stride());
     OpQ Q(job.q_stride());
-    typename JOB::Place here = job.place(n);
+    const int count = (end - n + step - 1) / step;       // tiles
+    int at = 0, table_at = 0;                              // the tile at work, the first of the table's
+    TileEntry table = job.entry(n + (int)(threadIdx.x % kWave) * step);
+    auto place = [&](int i) {
+      if (i - table_at >= kWave) {
+        table_at = at;
+        table = job.entry(n + (at + (int)(threadIdx.x % kWave)) * step);
+      }
+      TileEntry e;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e.v[j] = __builtin_amdgcn_readlane(table.v[j], i - table_at);
+      return job.place(e);
+    };
+    typename JOB::Place here = place(0);
     // the tiles that P's and Q's loads are at, and their chunks that are still to be loaded
-    int n_p = n, n_q = n, chunks_p = here.chunks(), chunks_q = chunks_p;
+    int at_p = 0, at_q = 0, chunks_p = here.chunks(), chunks_q = chunks_p;
     P.start(here.p, here.np, here.K);
     Q.start(here.q, here.nq, here.K);
     auto next_p = [&] {
       if (chunks_p == 0) {
-        n_p += step;
-        const typename JOB::Place place = n_p < end ? job.place(n_p) : JOB::Place::none(here);
-        P.start(place.p, place.np, place.K);
-        chunks_p = place.chunks();
+        const typename JOB::Place next = ++at_p < count ? place(at_p) : JOB::Place::none(here);
+        P.start(next.p, next.np, next.K);
+        chunks_p = next.chunks();
       }
       P.next();
       --chunks_p;
     };
     auto next_q = [&] {
       if (chunks_q == 0) {
-        n_q += step;
-        const typename JOB::Place place = n_q < end ? job.place(n_q) : JOB::Place::none(here);
-        Q.start(place.q, place.nq, place.K);
-        chunks_q = place.chunks();
+        const typename JOB::Place next = ++at_q < count ? place(at_q) : JOB::Place::none(here);
+        Q.start(next.q, next.nq, next.K);
+        chunks_q = next.chunks();
       }
       Q.next();
       --chunks_q;
@@ -344,9 +359,8 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
       }
       job.finish(here, *this);
       stores = true;
-      n += step;
-      if (n >= end) break;
-      here = job.place(n);
+      if (++at == count) break;
+      here = place(at);
     }
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // nothing is on its way to LDS when the workgroup ends
   }
@@ -502,11 +516,14 @@ template <typename DT, typename TILE, int BP, int BQ> struct ForwardJob {
 
   __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
   __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_in * kItem; }
-  __device__ __forceinline__ Place place(int n) const {
+  __device__ __forceinline__ TileEntry entry(int n) const {
     const RowTile t = tiles.find(n, ptiles);
-    const int p0 = t.column * BP;
-    return {w + ((int64_t)t.expert * d_out + p0) * d_in * kItem, x + (int64_t)t.first * d_in * kItem, min(BP, d_out - p0), t.rows,
-            d_in, TILE::OpP::kChunk, t.expert, t.first, p0};
+    return {{t.expert, t.first, t.rows, t.column * BP}};
+  }
+  __device__ __forceinline__ Place place(const TileEntry& t) const {
+    const int expert = t.v[0], first = t.v[1], nq = t.v[2], p0 = t.v[3];
+    return {w + ((int64_t)expert * d_out + p0) * d_in * kItem, x + (int64_t)first * d_in * kItem, min(BP, d_out - p0), nq, d_in,
+            TILE::OpP::kChunk, expert, first, p0};
   }
   __device__ __forceinline__ bool sums(const Place&) const { return false; }
   template <int ACT, bool KEEP> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
@@ -565,11 +582,14 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
 
   __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
   __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_out * kItem; }
-  __device__ __forceinline__ Place place(int n) const {
+  __device__ __forceinline__ TileEntry entry(int n) const {
     const RowTile t = tiles.find(n, ptiles);
-    const int p0 = t.column * BP;
-    return {w + ((int64_t)t.expert * d_out * d_in + p0) * kItem, grad_out + (int64_t)t.first * d_out * kItem, min(BP, d_in - p0),
-            t.rows, d_out, TILE::OpP::kChunk, t.expert, t.first, p0};
+    return {{t.expert, t.first, t.rows, t.column * BP}};
+  }
+  __device__ __forceinline__ Place place(const TileEntry& t) const {
+    const int expert = t.v[0], first = t.v[1], nq = t.v[2], p0 = t.v[3];
+    return {w + ((int64_t)expert * d_out * d_in + p0) * kItem, grad_out + (int64_t)first * d_out * kItem, min(BP, d_in - p0), nq,
+            d_out, TILE::OpP::kChunk, expert, first, p0};
   }
   __device__ __forceinline__ bool sums(const Place&) const { return false; }
   template <int ACT> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
@@ -637,17 +657,20 @@ template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
   static constexpr int kItem = ItemSize<DT>::value;
   const char *grad_out, *x;
   char *grad_w, *grad_bias;
-  int d_in, d_out, ptiles, qtiles;
-  const RowTiles& tiles;
+  const int32_t* offsets;
+  int rows, d_in, d_out, E, ptiles, qtiles;
 
   __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
   __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_out * kItem; }
-  __device__ __forceinline__ Place place(int n) const {
-    const int e = (int)((uint32_t)n / (uint32_t)(ptiles * qtiles)), inside = n - e * ptiles * qtiles;
-    const int q = (int)((uint32_t)inside / (uint32_t)ptiles), p0 = (inside - q * ptiles) * BP, q0 = q * BQ;
-    const RowRange range = tiles.range(e);
-    return {x + ((int64_t)range.lo * d_in + p0) * kItem, grad_out + ((int64_t)range.lo * d_out + q0) * kItem, min(BP, d_in - p0),
-            min(BQ, d_out - q0), range.hi - range.lo, e, p0, q0};
+  __device__ __forceinline__ TileEntry entry(int n) const {
+    const int e = min((int)((uint32_t)n / (uint32_t)(ptiles * qtiles)), E - 1);
+    const RowRange range = rows_of(offsets, e, rows);
+    return {{e, n - e * ptiles * qtiles, range.lo, range.hi - range.lo}};
+  }
+  __device__ __forceinline__ Place place(const TileEntry& t) const {
+    const int e = t.v[0], q = (int)((uint32_t)t.v[1] / (uint32_t)ptiles), p0 = (t.v[1] - q * ptiles) * BP, q0 = q * BQ;
+    return {x + ((int64_t)t.v[2] * d_in + p0) * kItem, grad_out + ((int64_t)t.v[2] * d_out + q0) * kItem, min(BP, d_in - p0),
+            min(BQ, d_out - q0), t.v[3], e, p0, q0};
   }
   __device__ __forceinline__ bool sums(const Place& at) const { return grad_bias != nullptr && at.p0 == 0; }
   __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
@@ -684,9 +707,8 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const ch
                                                                         const int32_t* __restrict__ offsets, int rows, int d_in,
                                                                         int d_out, int E, char* __restrict__ grad_w,
                                                                         char* __restrict__ grad_bias) {
-  const RowTiles tiles(offsets, E, rows, BQ);
   const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ;
-  const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, d_in, d_out, ptiles, qtiles, tiles};
+  const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, offsets, rows, d_in, d_out, E, ptiles, qtiles};
   const Share s = share_of_block(E * ptiles * qtiles);
   TILE tile;
   tile.run(job, s.first, s.end, s.step);

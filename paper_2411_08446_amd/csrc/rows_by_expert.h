@@ -29,70 +29,68 @@ struct RowTile {
 };
 
 // The experts' row tiles of `tile` rows, in the order of the experts.  Every wave counts them by itself: lane e % 64 has expert
-// e's, summed over the lanes.  The first 64 experts' counts stay in registers.
+// e's, summed over the lanes, 64 experts at a time.
 struct RowTiles {
   const int32_t* offsets;
   int rows, E, tile;
-  int lo, hi, upto;     // of expert `lane`: its rows, the tiles up to and with it
   int total;
 
-  __device__ __forceinline__ void count(int e0, int& lo_, int& hi_, int& upto_) const {
+  // Of expert e0 + lane: its rows, the tiles of experts e0 up to and with it.
+  __device__ __forceinline__ void count(int e0, int& lo, int& hi, int& upto) const {
     const int lane = (int)threadIdx.x % kWave;
     RowRange range = {0, 0};
     if (e0 + lane < E) range = rows_of(offsets, e0 + lane, rows);
-    lo_ = range.lo;
-    hi_ = range.hi;
-    upto_ = (hi_ - lo_ + tile - 1) / tile;
+    lo = range.lo;
+    hi = range.hi;
+    upto = (hi - lo + tile - 1) / tile;
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) {
-      const int below = __shfl_up(upto_, s, kWave);
-      if (lane >= s) upto_ += below;
+      const int below = __shfl_up(upto, s, kWave);
+      if (lane >= s) upto += below;
     }
   }
 
   __device__ __forceinline__ RowTiles(const int32_t* __restrict__ offsets_, int E_, int rows_, int tile_)
-      : offsets(offsets_), rows(rows_), E(E_), tile(tile_) {
-    count(0, lo, hi, upto);
-    total = __builtin_amdgcn_readlane(upto, kWave - 1);
-    for (int e0 = kWave; e0 < E; e0 += kWave) {
-      int l, h, u;
-      count(e0, l, h, u);
-      total += __builtin_amdgcn_readlane(u, kWave - 1);
+      : offsets(offsets_), rows(rows_), E(E_), tile(tile_), total(0) {
+    for (int e0 = 0; e0 < E; e0 += kWave) {
+      int lo, hi, upto;
+      count(e0, lo, hi, upto);
+      total += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
   }
 
-  // Rows of expert e.
-  __device__ __forceinline__ RowRange range(int e) const {
-    if (e < kWave) return {__builtin_amdgcn_readlane(lo, e), __builtin_amdgcn_readlane(hi, e)};
-    const RowRange r = rows_of(offsets, e, rows);
-    return {__builtin_amdgcn_readfirstlane(r.lo), __builtin_amdgcn_readfirstlane(r.hi)};
-  }
-
-  // Tile n < total * columns of the experts' row tiles by `columns` tiles of columns.  An expert's tiles go in bands of kBand row
-  // tiles, within a band column after column: the tiles that run at a time on an XCD are about as many rows as columns
-  // wide and share what they read (bands of 4: 3 % less time than row by row at 4096 -> 4096 columns).
+  // Tile n of the experts' row tiles by `columns` tiles of columns; every lane may ask for another one, and all lanes of a wave
+  // ask together (n >= total * columns gives anything).  An expert's tiles go in bands of kBand row tiles, within a band
+  // column after column: the tiles that run at a time on an XCD are about as many rows as columns wide and share what
+  // they read (bands of 4: 3 % less time than row by row at 4096 -> 4096 columns).
   __device__ __forceinline__ RowTile find(int n, int columns) const {
     constexpr int kBand = 4;
     const int m = (int)((uint32_t)n / (uint32_t)columns);
     int before = 0;                           // tiles of the experts below e0
-    int l = lo, h = hi, u = upto;
-    for (int e0 = 0;;) {
-      const uint64_t past = __ballot(before + u > m);
-      if (past != 0) {
-        const int at = __ffsll((unsigned long long)past) - 1;
-        const int rlo = __builtin_amdgcn_readlane(l, at), rhi = __builtin_amdgcn_readlane(h, at);
+    RowTile t = {0, 0, 0, 0};
+    for (int e0 = 0; e0 < E; e0 += kWave) {
+      int lo, hi, upto;
+      count(e0, lo, hi, upto);
+      const int here = __builtin_amdgcn_readlane(upto, kWave - 1);
+      int at = 0;                             // experts of these 64 that end at or before tile m
+#pragma unroll
+      for (int s = kWave / 2; s >= 1; s >>= 1)
+        if (before + __shfl(upto, at + s - 1, kWave) <= m) at += s;
+      at = min(at, kWave - 1);
+      const int rlo = __shfl(lo, at, kWave), rhi = __shfl(hi, at, kWave), past = __shfl(upto, at, kWave);
+      if (m >= before && m < before + here) {
         const int mine = (rhi - rlo + tile - 1) / tile;
-        const int inside = n - (before + __builtin_amdgcn_readlane(u, at) - mine) * columns;   // its number in the expert
+        const int inside = n - (before + past - mine) * columns;          // its number in the expert
         const int band = (int)((uint32_t)inside / (uint32_t)(kBand * columns)), rest = inside - band * kBand * columns;
         const int wide = min(kBand, mine - band * kBand);
-        const int column = (int)((uint32_t)rest / (uint32_t)wide), first = rlo + (band * kBand + rest - column * wide) * tile;
-        return {e0 + at, first, min(tile, rhi - first), column};
+        t.expert = e0 + at;
+        t.column = (int)((uint32_t)rest / (uint32_t)wide);
+        t.first = rlo + (band * kBand + rest - t.column * wide) * tile;
+        t.rows = min(tile, rhi - t.first);
       }
-      before += __builtin_amdgcn_readlane(u, kWave - 1);
-      e0 += kWave;
-      if (e0 >= E) return {0, 0, 0, 0};       // not reached for n < total * columns
-      count(e0, l, h, u);
+      before += here;
     }
+    return t;
   }
 };
 
