@@ -372,6 +372,8 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
   static constexpr int kSlots = ItemSize<DT>::value;        // 16-byte pieces of a lane per 32 x 32 results
   static constexpr int kStores = TP * TQ * kSlots;
 
+  static constexpr int kItemsPerWord = 4 / ItemSize<DT>::value;
+
   struct Lines {
     __amdgpu_buffer_rsrc_t buffer;
     uint32_t at, ld;     // the lane's first piece of the wave's part; bytes of a line
@@ -430,7 +432,8 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
         for (int i = 0; i < 4; ++i) swap16(w[4 * j + i], w[4 * j + 4 + i]);
     }
   }
-  __device__ __forceinline__ static void put(const Lines& l, int t, int u, const float (&v)[16]) {
+  struct Pieces { u32x4 v[kSlots]; };
+  __device__ __forceinline__ static Pieces pack(const float (&v)[16]) {
     uint32_t w[4 * kSlots];
     if constexpr (ItemSize<DT>::value == 2) {
 #pragma unroll
@@ -440,12 +443,16 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
       for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
     }
     exchange(w, false);
+    Pieces x;
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i)
-      __builtin_amdgcn_raw_buffer_store_b128((u32x4){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]}, l.buffer,
-                                             (int)piece_at(l, t, u, i), 0, 0);
+    for (int i = 0; i < kSlots; ++i) x.v[i] = (u32x4){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    return x;
   }
-  struct Pieces { u32x4 v[kSlots]; };
+  __device__ __forceinline__ static void put(const Lines& l, int t, int u, const Pieces& x) {
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) __builtin_amdgcn_raw_buffer_store_b128(x.v[i], l.buffer, (int)piece_at(l, t, u, i), 0, 0);
+  }
+  __device__ __forceinline__ static void put(const Lines& l, int t, int u, const float (&v)[16]) { put(l, t, u, pack(v)); }
   __device__ __forceinline__ static Pieces get(const Lines& l, int t, int u) {
     Pieces x;
 #pragma unroll
@@ -464,22 +471,29 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     }
   }
   // Four elements for each j of tile t from a line (bias); behind its end zeros.
-  __device__ __forceinline__ static void get_line(const char* line, int np, int t, float (&v)[16]) {
+  struct Fours { uint32_t v[4][4 / kItemsPerWord]; };
+  __device__ __forceinline__ static Fours get_line(const char* line, int np, int t) {
     const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)line, 0, np * ItemSize<DT>::value, 0x00020000);
+    Fours x;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int at = (wave % WP * TP * 32 + 32 * t + 8 * j + 4 * (lane / 32)) * ItemSize<DT>::value;
       if constexpr (ItemSize<DT>::value == 2) {
         const u32x2 q = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buffer, at, 0, 0));
-        v[4 * j] = __uint_as_float(q[0] << 16); v[4 * j + 1] = __uint_as_float(q[0] & 0xffff0000u);
-        v[4 * j + 2] = __uint_as_float(q[1] << 16); v[4 * j + 3] = __uint_as_float(q[1] & 0xffff0000u);
+        x.v[j][0] = q[0];
+        x.v[j][1] = q[1];
       } else {
         const u32x4 q = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, at, 0, 0));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * j + i] = __uint_as_float(q[i]);
+        for (int i = 0; i < 4; ++i) x.v[j][i] = q[i];
       }
     }
+    return x;
+  }
+  __device__ __forceinline__ static float four(const Fours& x, int i) {
+    const uint32_t w = x.v[i / 4][i % 4 / kItemsPerWord];
+    return __uint_as_float(ItemSize<DT>::value == 4 ? w : i % 2 ? w & 0xffff0000u : w << 16);
   }
 };
 
@@ -530,15 +544,21 @@ template <typename DT, typename TILE, int BP, int BQ> struct ForwardJob {
     const int64_t first = ((int64_t)at.first * d_out + at.p0) * kItem;
     const typename TILE::Lines o = TILE::lines(out + first, (uint32_t)d_out * kItem, at.nq, at.np);
     const typename TILE::Lines k = TILE::lines((KEEP ? pre : out) + first, (uint32_t)d_out * kItem, at.nq, at.np);
+    // all loads in front of the stores: operations count as done in their order, and a load behind a store would wait until
+    // that has reached memory
+    typename TILE::Fours b[TILE::TP] = {};
+    if (bias) {
+#pragma unroll
+      for (int t = 0; t < TILE::TP; ++t) b[t] = TILE::get_line(bias + ((int64_t)at.expert * d_out + at.p0) * kItem, at.np, t);
+      asm volatile("" : : : "memory");
+    }
 #pragma unroll
     for (int t = 0; t < TILE::TP; ++t) {
-      float b[16] = {};
-      if (bias) TILE::get_line(bias + ((int64_t)at.expert * d_out + at.p0) * kItem, at.np, t, b);
 #pragma unroll
       for (int u = 0; u < TILE::TQ; ++u) {
         float v[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i] + b[i];
+        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i] + TILE::four(b[t], i);
         if (KEEP) TILE::put(k, t, u, v);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = activate(v[i], ACT);
@@ -596,30 +616,46 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
     const int64_t first = ((int64_t)at.first * d_in + at.p0) * kItem;
     const typename TILE::Lines o = TILE::lines(grad_x + first, (uint32_t)d_in * kItem, at.nq, at.np);
     const typename TILE::Lines k = TILE::lines((ACT == LSHMOE_ACT_NONE ? grad_x : pre) + first, (uint32_t)d_in * kItem, at.nq, at.np);
-    // the values before the activation, a column tile ahead: a load waits for the stores in front of it
-    typename TILE::Pieces x[2][TILE::TQ];
-    auto get = [&](int t) {
+    // The values before the activation come in two halves, both loaded before anything is stored, as in the forward product; the
+    // first half's results wait, packed.
+    constexpr int kHalf = TILE::TP / 2;
+    typename TILE::Pieces x[kHalf][TILE::TQ], y[kHalf][TILE::TQ];
+    auto get = [&](int t0) {
 #pragma unroll
-      for (int u = 0; u < TILE::TQ; ++u) x[t & 1][u] = TILE::get(k, t, u);
+      for (int t = 0; t < kHalf; ++t)
+#pragma unroll
+        for (int u = 0; u < TILE::TQ; ++u) x[t][u] = TILE::get(k, t0 + t, u);
+      asm volatile("" : : : "memory");
+    };
+    auto scale = [&](int t0) {
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t)
+#pragma unroll
+        for (int u = 0; u < TILE::TQ; ++u) {
+          float v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = tile.acc[t0 + t][u][i];
+          if (ACT != LSHMOE_ACT_NONE) {
+            float z[16];
+            TILE::spread(x[t][u], z);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] *= activation_slope(z[i], ACT);
+          }
+          y[t][u] = TILE::pack(v);
+        }
+    };
+    auto put = [&](int t0) {
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t)
+#pragma unroll
+        for (int u = 0; u < TILE::TQ; ++u) TILE::put(o, t0 + t, u, y[t][u]);
     };
     if (ACT != LSHMOE_ACT_NONE) get(0);
-#pragma unroll
-    for (int t = 0; t < TILE::TP; ++t) {
-      if (ACT != LSHMOE_ACT_NONE && t + 1 < TILE::TP) get(t + 1);
-#pragma unroll
-      for (int u = 0; u < TILE::TQ; ++u) {
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i];
-        if (ACT != LSHMOE_ACT_NONE) {
-          float z[16];
-          TILE::spread(x[t & 1][u], z);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] *= activation_slope(z[i], ACT);
-        }
-        TILE::put(o, t, u, v);
-      }
-    }
+    scale(0);
+    if (ACT != LSHMOE_ACT_NONE) get(kHalf);
+    put(0);
+    scale(kHalf);
+    put(kHalf);
   }
   __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
     if (act == LSHMOE_ACT_RELU) store<LSHMOE_ACT_RELU>(at, tile);

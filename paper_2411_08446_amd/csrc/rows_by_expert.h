@@ -94,15 +94,36 @@ struct RowTiles {
   }
 };
 
+// The normal distribution beyond u >= 0, Q(u) = integral of phi from u on, and phi(u).  Q(u) = exp(-u^2 / 2) P(t), t = 1 / (1 + p u),
+// P of degree 5 without a constant term: the form of Abramowitz and Stegun 26.2.17, with p and coefficients fitted for the
+// least maximum error, 6.1e-8.  Evaluated in binary32 it is good to 2.1e-7 (the library's erf takes twice as long, which at
+// K = 1024 was a quarter of a product's time).
+struct NormalTail { float beyond, density; };
+__device__ __forceinline__ NormalTail normal_tail(float u) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.331f, u, 1.0f));
+  const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752f);
+  float p = fmaf(-0.110234566f, t, 0.374119867f);
+  p = fmaf(p, t, -0.0900151826f);
+  p = fmaf(p, t, 0.203860818f);
+  p = fmaf(p, t, 0.122269003f);
+  return {e * (p * t), e * 0.39894228f};
+}
+
 __device__ __forceinline__ float activate(float v, int act) {
-  if (act == LSHMOE_ACT_RELU) return v > 0.0f || v != v ? v : 0.0f;
-  if (act == LSHMOE_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
+  if (act == LSHMOE_ACT_RELU) return v < 0.0f ? 0.0f : v;
+  if (act == LSHMOE_ACT_GELU) {
+    const float u = fminf(fabsf(v), 64.0f);       // infinities: 64 is as good
+    return fmaf(-u, normal_tail(u).beyond, v < 0.0f ? 0.0f : v);
+  }
   return v;
 }
 
 __device__ __forceinline__ float activation_slope(float v, int act) {
   if (act == LSHMOE_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
-  if (act == LSHMOE_ACT_GELU) return 0.5f * (1.0f + erff(v * 0.70710678f)) + v * expf(-0.5f * v * v) * 0.39894228f;
+  if (act == LSHMOE_ACT_GELU) {
+    const NormalTail n = normal_tail(fminf(fabsf(v), 64.0f));
+    return fmaf(v, n.density, v < 0.0f ? n.beyond : 1.0f - n.beyond);
+  }
   return 1.0f;
 }
 
