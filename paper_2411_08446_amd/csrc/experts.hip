@@ -366,13 +366,12 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
   }
 
   // ---- results: lanes and memory.  Of the 32 x 32 results of tiles t, u a lane has q = r = lane % 32 and, h = lane / 32, p = 8 j + 4 h
-  // + 0 .. 3 for j = 0 .. 3.  Two exchanges between lanes make that 16 bytes of consecutive p to a lane, 64 bytes of 16 rows to
-  // an instruction: lane l then has q = 16 i + l % 16 and the piece number piece(l), i = 0, 1 (bf16; four of 16 bytes in
-  // binary32: two times 16 q by two times 64 bytes).
-  static constexpr int kSlots = ItemSize<DT>::value;        // 16-byte pieces of a lane per 32 x 32 results
-  static constexpr int kStores = TP * TQ * kSlots;
-
+  // + 0 .. 3 for j = 0 .. 3.  Three exchanges between lanes make that 16 bytes of consecutive p to a lane and whole lines of 128
+  // bytes of 8 rows to an instruction: a group, 128 bytes of p (one tile of binary32, two of bf16) by 32 q, is four pieces
+  // to a lane, of q = 8 i + lane % 8.  (64 bytes of 16 rows: 13 % more time at K = 1024 with two results stored.)
   static constexpr int kItemsPerWord = 4 / ItemSize<DT>::value;
+  static constexpr int kGroupTiles = kItemsPerWord, kGroups = TP / kGroupTiles;
+  static constexpr int kStores = kGroups * TQ * 4;
 
   struct Lines {
     __amdgpu_buffer_rsrc_t buffer;
@@ -386,16 +385,17 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     Lines l;
     l.buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
     l.ld = ld;
-    l.p = wave % WP * TP * 32 + (ItemSize<DT>::value == 2 ? 16 * (lane / 16 % 2) + 8 * (lane / 32) : 8 * (lane / 16 % 2) + 4 * (lane / 32));
+    l.p = wave % WP * TP * 32 + (lane / 8 % 2 * 32 + lane / 16 % 2 * 16 + lane / 32 * 8) * kItemsPerWord / 2;
     l.np = np;
-    l.at = (uint32_t)(wave / WP * TQ * 32 + lane % 16) * ld + (uint32_t)l.p * ItemSize<DT>::value;
+    l.at = (uint32_t)(wave / WP * TQ * 32 + lane % 8) * ld + (uint32_t)l.p * ItemSize<DT>::value;
     return l;
   }
-  // Offset of the lane's piece i of tiles t, u; behind the end of the buffer where there is no such column (or line).
-  __device__ __forceinline__ static uint32_t piece_at(const Lines& l, int t, int u, int i) {
-    const int column = 32 * t + (ItemSize<DT>::value == 2 ? 0 : i / 2 * 16), line = 32 * u + i % 2 * 16;
-    return l.p + column < l.np ? l.at + (uint32_t)line * l.ld + (uint32_t)column * ItemSize<DT>::value : kNowhere;
+  // Offset of the lane's piece i of group g and tile u; behind the end of the buffer where there is no such column (or line).
+  __device__ __forceinline__ static uint32_t piece_at(const Lines& l, int g, int u, int i) {
+    return l.p + 32 * kGroupTiles * g < l.np ? l.at + (uint32_t)(32 * u + 8 * i) * l.ld + 128u * g : kNowhere;
   }
+  // Lanes 32 .. 63 of x and 0 .. 31 of y change places; lanes 16 .. 31 of 32 of x and 0 .. 15 of y; lanes 8 .. 15 of 16 of x and 0 .. 7
+  // of y.  Each is its own inverse.
   __device__ __forceinline__ static void swap32(uint32_t& x, uint32_t& y) {
     const auto v = __builtin_amdgcn_permlane32_swap(x, y, false, false);
     x = v[0];
@@ -406,69 +406,86 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     x = v[0];
     y = v[1];
   }
-  // The exchanges, their own inverse.  bf16: w[2 j + i] is the pair of p 8 j + 4 h + 2 i; piece i afterwards w[4 i .. 4 i + 3].
-  // binary32: w[4 j + i] is p 8 j + 4 h + i; piece i afterwards w[4 i .. 4 i + 3].
-  __device__ __forceinline__ static void exchange(uint32_t (&w)[4 * kSlots], bool back) {
-    if constexpr (ItemSize<DT>::value == 2) {
-      // w[0..3]: j = 0, 1; the pieces want {w0 w1 | w2 w3} with the halves joined
-      if (!back) {
-        swap32(w[0], w[2]);
-        swap32(w[1], w[3]);
-        swap32(w[4], w[6]);
-        swap32(w[5], w[7]);
-      }
+  __device__ __forceinline__ static void swap8(uint32_t& x, uint32_t& y) {
+    constexpr int kRotateBy8 = 0x128;
+    const uint32_t a = (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)y, kRotateBy8, 0xf, 0xc, false);
+    y = (uint32_t)__builtin_amdgcn_update_dpp((int)y, (int)x, kRotateBy8, 0xf, 0x3, false);
+    x = a;
+  }
+  // From the lanes' results to pieces, w[4 i .. 4 i + 3] piece i, or back.  Before: bf16 w[8 t + 2 j + i] is the pair of p 32 t + 8 j + 4 h +
+  // 2 i, binary32 w[4 j + i] is p 8 j + 4 h + i.
+  __device__ __forceinline__ static void exchange(uint32_t (&w)[16], bool back) {
+    auto halves = [&] {
+      if (ItemSize<DT>::value != 2) return;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) swap16(w[i], w[4 + i]);
-      if (back) {
-        swap32(w[0], w[2]);
-        swap32(w[1], w[3]);
-        swap32(w[4], w[6]);
-        swap32(w[5], w[7]);
+      for (int i = 0; i < 16; i += 4) {
+        swap32(w[i], w[i + 2]);
+        swap32(w[i + 1], w[i + 3]);
       }
+    };
+    auto rows16 = [&] {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        swap16(w[i], w[4 + i]);
+        swap16(w[8 + i], w[12 + i]);
+      }
+    };
+    auto rows8 = [&] {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        swap8(w[i], w[8 + i]);
+        swap8(w[4 + i], w[12 + i]);
+      }
+    };
+    if (!back) {
+      halves();
+      rows16();
+      rows8();
     } else {
-#pragma unroll
-      for (int j = 0; j < 4; j += 2)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) swap16(w[4 * j + i], w[4 * j + 4 + i]);
+      rows8();
+      rows16();
+      halves();
     }
   }
-  struct Pieces { u32x4 v[kSlots]; };
-  __device__ __forceinline__ static Pieces pack(const float (&v)[16]) {
-    uint32_t w[4 * kSlots];
-    if constexpr (ItemSize<DT>::value == 2) {
+  struct Pieces { u32x4 v[4]; };
+  // A group's pieces of results v, element 16 t + 4 j + i.  Pieces 1 and 2 come out of the exchanges in each other's place.
+  __device__ __forceinline__ static Pieces pack(const float (&v)[16 * kGroupTiles]) {
+    uint32_t w[16];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = f32_to_bf16_pair(v[2 * i], v[2 * i + 1]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (ItemSize<DT>::value == 2) w[i] = f32_to_bf16_pair(v[2 * i], v[2 * i + 1]);
+      else w[i] = __float_as_uint(v[i]);
     }
     exchange(w, false);
     Pieces x;
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) x.v[i] = (u32x4){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    for (int i = 0; i < 4; ++i) x.v[i % 2 * 2 + i / 2] = (u32x4){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
     return x;
   }
-  __device__ __forceinline__ static void put(const Lines& l, int t, int u, const Pieces& x) {
+  __device__ __forceinline__ static void put(const Lines& l, int g, int u, const Pieces& x) {
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) __builtin_amdgcn_raw_buffer_store_b128(x.v[i], l.buffer, (int)piece_at(l, t, u, i), 0, 0);
+    for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b128(x.v[i], l.buffer, (int)piece_at(l, g, u, i), 0, 0);
   }
-  __device__ __forceinline__ static void put(const Lines& l, int t, int u, const float (&v)[16]) { put(l, t, u, pack(v)); }
-  __device__ __forceinline__ static Pieces get(const Lines& l, int t, int u) {
+  __device__ __forceinline__ static Pieces get(const Lines& l, int g, int u) {
     Pieces x;
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.buffer, (int)piece_at(l, t, u, i), 0, 0));
+    for (int i = 0; i < 4; ++i) x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.buffer, (int)piece_at(l, g, u, i), 0, 0));
     return x;
   }
-  __device__ __forceinline__ static void spread(const Pieces& x, float (&v)[16]) {
-    uint32_t w[4 * kSlots];
+  __device__ __forceinline__ static void spread(const Pieces& x, float (&v)[16 * kGroupTiles]) {
+    uint32_t w[16];
 #pragma unroll
-    for (int i = 0; i < 4 * kSlots; ++i) w[i] = x.v[i / 4][i % 4];
+    for (int i = 0; i < 16; ++i) w[i] = x.v[i / 4 % 2 * 2 + i / 8][i % 4];
     exchange(w, true);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 16 * kGroupTiles; ++i) {
       if constexpr (ItemSize<DT>::value == 2) v[i] = __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
       else v[i] = __uint_as_float(w[i]);
     }
+  }
+  __device__ __forceinline__ void results(int g, int u, float (&v)[16 * kGroupTiles]) const {
+#pragma unroll
+    for (int i = 0; i < 16 * kGroupTiles; ++i) v[i] = acc[g * kGroupTiles + i / 16][u][i % 16];
   }
   // Four elements for each j of tile t from a line (bias); behind its end zeros.
   struct Fours { uint32_t v[4][4 / kItemsPerWord]; };
@@ -553,16 +570,17 @@ template <typename DT, typename TILE, int BP, int BQ> struct ForwardJob {
       asm volatile("" : : : "memory");
     }
 #pragma unroll
-    for (int t = 0; t < TILE::TP; ++t) {
+    for (int g = 0; g < TILE::kGroups; ++g) {
 #pragma unroll
       for (int u = 0; u < TILE::TQ; ++u) {
-        float v[16];
+        float v[16 * TILE::kGroupTiles];
+        tile.results(g, u, v);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i] + TILE::four(b[t], i);
-        if (KEEP) TILE::put(k, t, u, v);
+        for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] += TILE::four(b[g * TILE::kGroupTiles + i / 16], i % 16);
+        if (KEEP) TILE::put(k, g, u, TILE::pack(v));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = activate(v[i], ACT);
-        TILE::put(o, t, u, v);
+        for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] = activate(v[i], ACT);
+        TILE::put(o, g, u, TILE::pack(v));
       }
     }
   }
@@ -618,37 +636,37 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
     const typename TILE::Lines k = TILE::lines((ACT == LSHMOE_ACT_NONE ? grad_x : pre) + first, (uint32_t)d_in * kItem, at.nq, at.np);
     // The values before the activation come in two halves, both loaded before anything is stored, as in the forward product; the
     // first half's results wait, packed.
-    constexpr int kHalf = TILE::TP / 2;
+    constexpr int kHalf = TILE::kGroups / 2;
     typename TILE::Pieces x[kHalf][TILE::TQ], y[kHalf][TILE::TQ];
-    auto get = [&](int t0) {
+    auto get = [&](int g0) {
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t)
+      for (int g = 0; g < kHalf; ++g)
 #pragma unroll
-        for (int u = 0; u < TILE::TQ; ++u) x[t][u] = TILE::get(k, t0 + t, u);
+        for (int u = 0; u < TILE::TQ; ++u) x[g][u] = TILE::get(k, g0 + g, u);
       asm volatile("" : : : "memory");
     };
-    auto scale = [&](int t0) {
+    auto scale = [&](int g0) {
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t)
+      for (int g = 0; g < kHalf; ++g)
 #pragma unroll
         for (int u = 0; u < TILE::TQ; ++u) {
-          float v[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = tile.acc[t0 + t][u][i];
+          constexpr int kElems = 16 * TILE::kGroupTiles;
+          float v[kElems];
+          tile.results(g0 + g, u, v);
           if (ACT != LSHMOE_ACT_NONE) {
-            float z[16];
-            TILE::spread(x[t][u], z);
+            float z[kElems];
+            TILE::spread(x[g][u], z);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] *= activation_slope(z[i], ACT);
+            for (int i = 0; i < kElems; ++i) v[i] *= activation_slope(z[i], ACT);
           }
-          y[t][u] = TILE::pack(v);
+          y[g][u] = TILE::pack(v);
         }
     };
-    auto put = [&](int t0) {
+    auto put = [&](int g0) {
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t)
+      for (int g = 0; g < kHalf; ++g)
 #pragma unroll
-        for (int u = 0; u < TILE::TQ; ++u) TILE::put(o, t0 + t, u, y[t][u]);
+        for (int u = 0; u < TILE::TQ; ++u) TILE::put(o, g0 + g, u, y[g][u]);
     };
     if (ACT != LSHMOE_ACT_NONE) get(0);
     scale(0);
@@ -713,13 +731,12 @@ template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
     const typename TILE::Lines o = TILE::lines(grad_w + (((int64_t)at.expert * d_out + at.q0) * d_in + at.p0) * kItem,
                                                (uint32_t)d_in * kItem, at.nq, at.np);
 #pragma unroll
-    for (int t = 0; t < TILE::TP; ++t)
+    for (int g = 0; g < TILE::kGroups; ++g)
 #pragma unroll
       for (int u = 0; u < TILE::TQ; ++u) {
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = tile.acc[t][u][i];
-        TILE::put(o, t, u, v);
+        float v[16 * TILE::kGroupTiles];
+        tile.results(g, u, v);
+        TILE::put(o, g, u, TILE::pack(v));
       }
     if (!sums(at)) return;
     // the waves of one column of waves have the same Q: the first stores, the lane halves' sums joined
