@@ -53,11 +53,12 @@ template <> __device__ __forceinline__ void mma<F32>(const u32x4& a, const u32x4
   c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[3]), __uint_as_float(b[3]), c, 0, 0, 0);
 }
 
-// 16 bytes per lane from a buffer straight into LDS: lane l's piece lands at dst + 16 l (dst is wave-uniform); a lane whose
-// offset is behind the buffer's end gets zeros.  Inline assembly, because behind the compiler's own builtin every LDS read
+// 16 bytes per lane from a buffer straight into LDS: lane l's piece, offset + ahead bytes into the buffer, lands at dst + 16 l (ahead
+// and dst are wave-uniform); a lane whose piece is behind the buffer's end gets zeros.  Inline assembly, because behind the compiler's own builtin every LDS read
 // waits until the load has landed; the caller waits for these loads itself.
-__device__ __forceinline__ void load16_to_lds(const i32x4& buffer, uint32_t offset, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(offset), "s"(dst), "s"(buffer) : "memory", "m0");
+__device__ __forceinline__ void load16_to_lds(const i32x4& buffer, uint32_t offset, uint32_t ahead, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
+               : : "v"(offset), "s"(dst), "s"(buffer), "s"(ahead) : "memory", "m0");
 }
 
 __device__ __forceinline__ i32x4 buffer_of(const char* base, int64_t bytes) {
@@ -84,12 +85,14 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
   uint32_t offset[kLoads];   // of the lane's pieces from the chunk's first element
   uint32_t k_piece;          // rows: the lane's piece within the chunk, in bytes
   uint32_t stride;           // bytes from one index (rows) or k (columns) to the next
-  // what is loaded next
-  const char* base;          // its first element
-  int64_t bytes;             // from there to the end of what may be read
-  int left;                  // rows: bytes of k from there on
-  i32x4 buffer;              // descriptor of the chunk being loaded
-  bool cut;                  // the lane's piece of it is behind the end of the rows
+  i32x4 buffer;              // descriptor of what may be read from the tile's first element (or from further on) to its end
+  uint32_t ahead;            // of the next chunk's first element from there
+  uint32_t now;              // of the chunk being loaded
+  int left;                  // rows: bytes of k from the next chunk on
+  bool tail;                 // the chunk being loaded is not a whole one
+  bool cut;                  // the lane's piece of a chunk that is not whole is behind the end of the rows
+  const char* base;          // columns: where the buffer starts, the bytes to its end
+  int64_t bytes;
 
   __device__ __forceinline__ explicit Operand(uint32_t stride_) : k_piece(0), stride(stride_) {
     const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
@@ -113,21 +116,31 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
     left = K * kItem;
     bytes = COLUMNS ? (int64_t)(K - 1) * stride + indices * kItem : (int64_t)(indices - 1) * stride + K * kItem;
     if (K == 0 || indices == 0) bytes = 0;
+    cut = !COLUMNS && (int)k_piece >= left % kChunkBytes;
+    restart();
   }
-  // Prepares the loads of the next chunk.  Behind the last one the loads bring zeros and read nothing.
-  __device__ __forceinline__ void next() {
+  __device__ __forceinline__ void restart() {
     buffer = buffer_of(base, bytes);
+    ahead = 0;
     // the descriptor may come from vector instructions: five cycles before its use
     asm volatile("s_nop 4" : "+s"(buffer));
-    cut = !COLUMNS && (int)k_piece >= left;
-    const int64_t step = COLUMNS ? (int64_t)kChunk * stride : kChunkBytes;
-    base += step;
-    bytes -= step;
+  }
+  // The next chunk's loads begin.  Behind the last chunk they bring zeros and read nothing.
+  __device__ __forceinline__ void next() {
+    if (COLUMNS && ahead >= 1u << 30) {             // offsets are 32 bits and a buffer ends below 2^31
+      base += ahead;
+      bytes -= ahead;
+      restart();
+    }
+    now = ahead;
+    ahead += COLUMNS ? kChunk * stride : (uint32_t)kChunkBytes;
+    tail = !COLUMNS && left < kChunkBytes;
     left -= kChunkBytes;
   }
   // Starts load i of the chunk; lds: where the ring's slot has the wave's first 1024 bytes.
   __device__ __forceinline__ void load(int i, uint32_t lds) const {
-    load16_to_lds(buffer, cut ? kNowhere : offset[i], lds + i * WAVES * 1024);
+    if (tail) load16_to_lds(buffer, cut ? kNowhere : offset[i], now, lds + i * WAVES * 1024);
+    else load16_to_lds(buffer, offset[i], now, lds + i * WAVES * 1024);
   }
 };
 
@@ -232,12 +245,6 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
       lds_char* const from_q = s == kSteps - 1 ? next_q_at : now_q;
       static_for<2>([&](auto hc) {
         constexpr int half = decltype(hc)::value;
-        if (s == 3 && half == 0) next_q();
-        if (s == 3) Q.load(half, to_q + slot_q * OpQ::kBytes);
-        if (s == 0 && !first) Q.load(2 + half, to_q + (slot_q ^ 1) * OpQ::kBytes);
-        if (s == 1 && half == 0) next_p();
-        if (s == 1 || s == 2) P.load(2 * (s - 1) + half, to_p + slot_free * OpP::kBytes);
-        __builtin_amdgcn_sched_barrier(0);
         // the fragments of the next step are on their way while this one's products run
 #pragma unroll
         for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t) a[then][t] = fp.read(from_p, sn, t);
@@ -261,6 +268,13 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
           __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / kTurns - kProducts * n / kTurns, 0);
         });
         __builtin_amdgcn_sched_barrier(0);
+        // one load, in the shadow of the products just started
+        if (s == 3 && half == 0) next_q();
+        if (s == 3) Q.load(half, to_q + slot_q * OpQ::kBytes);
+        if (s == 0 && !first) Q.load(2 + half, to_q + (slot_q ^ 1) * OpQ::kBytes);
+        if (s == 1 && half == 0) next_p();
+        if (s == 1 || s == 2) P.load(2 * (s - 1) + half, to_p + slot_free * OpP::kBytes);
+        __builtin_amdgcn_sched_barrier(0);
       });
     });
     if (last) {
@@ -273,8 +287,8 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
 
   // The tiles n, n + step, .. below end.  JOB: entry(n) says which tile n is, each lane of another one; place(entry) gives a
   // tile's operands and where its results go; finish(place, tile) stores them, with kStores stores to a wave or more.
-  // Lane i of a wave has the entry of the tile i steps on: looked up one by one, between the products, they cost
-  // 7 of a tile's 40 us at K = 1024.
+  // Lane i of a wave has the entry of the tile i steps on: looked up one by one between the products, they cost
+  // 3 of a tile's 40 us at K = 1024.
   template <typename JOB> __device__ __forceinline__ void run(const JOB& job, int n, int end, int step) {
     extern __shared__ uint4 lds[];
     if (n >= end) return;
