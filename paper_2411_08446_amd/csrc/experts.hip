@@ -89,8 +89,8 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
   uint32_t ahead;            // of the next chunk's first element from there
   uint32_t now;              // of the chunk being loaded
   int left;                  // rows: bytes of k from the next chunk on
-  bool tail;                 // the chunk being loaded is not a whole one
-  bool cut;                  // the lane's piece of a chunk that is not whole is behind the end of the rows
+  uint32_t cut;              // rows: kNowhere where the lane's piece of a chunk that is not whole is behind the end of the rows
+  uint32_t away;             // the same for the chunk being loaded
   const char* base;          // columns: where the buffer starts, the bytes to its end
   int64_t bytes;
 
@@ -116,7 +116,7 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
     left = K * kItem;
     bytes = COLUMNS ? (int64_t)(K - 1) * stride + indices * kItem : (int64_t)(indices - 1) * stride + K * kItem;
     if (K == 0 || indices == 0) bytes = 0;
-    cut = !COLUMNS && (int)k_piece >= left % kChunkBytes;
+    cut = !COLUMNS && (int)k_piece >= left % kChunkBytes ? kNowhere : 0u;
     restart();
   }
   __device__ __forceinline__ void restart() {
@@ -134,13 +134,13 @@ template <typename DT, bool COLUMNS, int B, int WAVES> struct Operand {
     }
     now = ahead;
     ahead += COLUMNS ? kChunk * stride : (uint32_t)kChunkBytes;
-    tail = !COLUMNS && left < kChunkBytes;
+    if (!COLUMNS) away = left < kChunkBytes ? cut : 0u;
     left -= kChunkBytes;
+    asm volatile("s_nop 4" : "+s"(buffer), "+s"(now));   // as in restart
   }
   // Starts load i of the chunk; lds: where the ring's slot has the wave's first 1024 bytes.
   __device__ __forceinline__ void load(int i, uint32_t lds) const {
-    if (tail) load16_to_lds(buffer, cut ? kNowhere : offset[i], now, lds + i * WAVES * 1024);
-    else load16_to_lds(buffer, offset[i], now, lds + i * WAVES * 1024);
+    load16_to_lds(buffer, COLUMNS ? offset[i] : offset[i] | away, now, lds + i * WAVES * 1024);
   }
 };
 
@@ -221,10 +221,10 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
   // c + 2 (two behind the barrier of chunk c, two in step 0 of chunk c + 1) and P's chunk c + 3 (steps 1 and 2); at a tile's
   // last chunk all of Q's are started before the results' stores, and its successor skips them.
   // kBehind: vector-memory operations that a wave may have started behind the loads that the barrier stands for.
-  template <bool SUMS, typename NextP, typename NextQ>
+  template <bool SUMS, bool FIRST, bool LAST, typename NextP, typename NextQ>
   __device__ __forceinline__ void chunk(const Fragments<DT, P_COLUMNS, BP, TP>& fp, const Fragments<DT, Q_COLUMNS, BQ, TQ>& fq,
                                         OpP& P, OpQ& Q, NextP&& next_p, NextQ&& next_q, lds_char* base, uint32_t to_p,
-                                        uint32_t to_q, int& slot_p, int& slot_q, bool first, bool last, bool stores) {
+                                        uint32_t to_q, int& slot_p, int& slot_q, bool stores) {
     lds_char* const now_p = base + slot_p * OpP::kBytes;
     lds_char* const now_q = base + kAtQ + slot_q * OpQ::kBytes;
     const int slot_next = slot_p == kRingP - 1 ? 0 : slot_p + 1, slot_free = slot_p == 0 ? kRingP - 1 : slot_p - 1;
@@ -236,7 +236,7 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
         // The last fragments of this chunk are in registers, this wave's share of the next one has landed (P's of the one after it and a
         // finished tile's stores may be under way).  Behind the barrier that is so for all waves: this chunk's slots are
         // free, the next one may be read.
-        if (stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(4 + kStores) : "memory");
+        if (FIRST && stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(4 + kStores) : "memory");
         else asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" : : : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" : : : "memory");
@@ -271,18 +271,33 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
         // one load, in the shadow of the products just started
         if (s == 3 && half == 0) next_q();
         if (s == 3) Q.load(half, to_q + slot_q * OpQ::kBytes);
-        if (s == 0 && !first) Q.load(2 + half, to_q + (slot_q ^ 1) * OpQ::kBytes);
+        if (s == 0 && !FIRST) Q.load(2 + half, to_q + (slot_q ^ 1) * OpQ::kBytes);
         if (s == 1 && half == 0) next_p();
         if (s == 1 || s == 2) P.load(2 * (s - 1) + half, to_p + slot_free * OpP::kBytes);
         __builtin_amdgcn_sched_barrier(0);
       });
     });
-    if (last) {
+    if (LAST) {
       Q.load(2, to_q + slot_q * OpQ::kBytes);
       Q.load(3, to_q + slot_q * OpQ::kBytes);
     }
     slot_p = slot_next;
     slot_q ^= 1;
+  }
+
+  // All chunks of a tile.
+  template <bool SUMS, typename NextP, typename NextQ>
+  __device__ __forceinline__ void products(const Fragments<DT, P_COLUMNS, BP, TP>& fp, const Fragments<DT, Q_COLUMNS, BQ, TQ>& fq,
+                                           OpP& P, OpQ& Q, NextP&& next_p, NextQ&& next_q, lds_char* base, uint32_t to_p,
+                                           uint32_t to_q, int& slot_p, int& slot_q, int chunks, bool stores) {
+    if (chunks == 1) {
+      chunk<SUMS, true, true>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, stores);
+      return;
+    }
+    chunk<SUMS, true, false>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, stores);
+    for (int c = chunks - 2; c > 0; --c)
+      chunk<SUMS, false, false>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, stores);
+    chunk<SUMS, false, true>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, stores);
   }
 
   // The tiles n, n + step, .. below end.  JOB: entry(n) says which tile n is, each lane of another one; place(entry) gives a
@@ -363,14 +378,8 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
         for (int t = 0; t < TP; ++t) acc[t][u] = (f32x16){};
         sums[u] = 0.0f;
       }
-      const int chunks = here.chunks();
-      if (JOB::kSums && job.sums(here)) {
-        for (int c = 0; c < chunks; ++c)
-          chunk<JOB::kSums>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, c == 0, c == chunks - 1, stores && c == 0);
-      } else {
-        for (int c = 0; c < chunks; ++c)
-          chunk<false>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, c == 0, c == chunks - 1, stores && c == 0);
-      }
+      if (JOB::kSums && job.sums(here)) products<JOB::kSums>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, here.chunks(), stores);
+      else products<false>(fp, fq, P, Q, next_p, next_q, base, to_p, to_q, slot_p, slot_q, here.chunks(), stores);
       job.finish(here, *this);
       stores = true;
       if (++at == count) break;
