@@ -207,7 +207,7 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
 
   f32x16 acc[TP][TQ];
   float sums[TQ];           // where wanted: Q summed over the k that the lane half holds
-  u32x4 a[2][TP], b[2][TQ]; // fragments of a step and of the one after it
+  u32x4 a[2][TP / 2], b[2][TQ];   // fragments: of half a step and the next half; of a step and the next one
 
   __device__ __forceinline__ static void add_elements(const u32x4& q, float& sum) {
 #pragma unroll
@@ -217,10 +217,10 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     }
   }
 
-  // One chunk's products, the loads of chunks ahead, the fragments of the next chunk's first step.  Loads in the order Q's chunk
-  // c + 2 (two behind the barrier of chunk c, two in step 0 of chunk c + 1) and P's chunk c + 3 (steps 1 and 2); at a tile's
-  // last chunk all of Q's are started before the results' stores, and its successor skips them.
-  // kBehind: vector-memory operations that a wave may have started behind the loads that the barrier stands for.
+  // One chunk's products, the loads of chunks ahead, the first fragments of the next chunk.  A half step is the products of half
+  // of P's tiles: fragments of P are read half a step ahead, of Q a step ahead.  In front of the last half step is the
+  // chunk's barrier.  Loads, one to a half step: Q's chunk c + 2 behind the barrier of chunk c, then P's chunk c + 3; at a
+  // tile's last chunk all of Q's are started before the results' stores, and its successor skips them.
   template <bool SUMS, bool FIRST, bool LAST, typename NextP, typename NextQ>
   __device__ __forceinline__ void chunk(const Fragments<DT, P_COLUMNS, BP, TP>& fp, const Fragments<DT, Q_COLUMNS, BQ, TQ>& fq,
                                         OpP& P, OpQ& Q, NextP&& next_p, NextQ&& next_q, lds_char* base, uint32_t to_p,
@@ -230,9 +230,10 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     const int slot_next = slot_p == kRingP - 1 ? 0 : slot_p + 1, slot_free = slot_p == 0 ? kRingP - 1 : slot_p - 1;
     lds_char* const next_p_at = base + slot_next * OpP::kBytes;
     lds_char* const next_q_at = base + kAtQ + (slot_q ^ 1) * OpQ::kBytes;
-    static_for<kSteps>([&](auto sc) {
-      constexpr int s = decltype(sc)::value, now = s & 1, then = now ^ 1, sn = (s + 1) % kSteps;
-      if (s == kSteps - 1) {
+    static_for<2 * kSteps>([&](auto ic) {
+      constexpr int i = decltype(ic)::value, s = i / 2, half = i % 2;
+      constexpr bool kEnd = i == 2 * kSteps - 1;
+      if (kEnd) {
         // The last fragments of this chunk are in registers, this wave's share of the next one has landed (P's of the one after it and a
         // finished tile's stores may be under way).  Behind the barrier that is so for all waves: this chunk's slots are
         // free, the next one may be read.
@@ -241,46 +242,48 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
         __builtin_amdgcn_s_barrier();
         asm volatile("" : : : "memory");
       }
-      lds_char* const from_p = s == kSteps - 1 ? next_p_at : now_p;
-      lds_char* const from_q = s == kSteps - 1 ? next_q_at : now_q;
-      static_for<2>([&](auto hc) {
-        constexpr int half = decltype(hc)::value;
-        // the fragments of the next step are on their way while this one's products run
+      // reads for the next half step
+      constexpr int sn = kEnd ? 0 : (i + 1) / 2, halfn = (i + 1) % 2;
 #pragma unroll
-        for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t) a[then][t] = fp.read(from_p, sn, t);
+      for (int t = 0; t < TP / 2; ++t) a[halfn][t] = fp.read(kEnd ? next_p_at : now_p, sn, halfn * TP / 2 + t);
+      constexpr int kFirstQ = kEnd ? 0 : s == kSteps - 1 ? TQ : half * TQ / 2;
+      constexpr int kLastQ = kEnd ? TQ : s == kSteps - 1 ? TQ : (half + 1) * TQ / 2;
 #pragma unroll
-        for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) b[then][u] = fq.read(from_q, sn, u);
+      for (int u = kFirstQ; u < kLastQ; ++u) b[(s + 1) & 1][u] = fq.read(kEnd ? next_q_at : now_q, (s + 1) % kSteps, u);
 #pragma unroll
-        for (int t = half * TP / 2; t < (half + 1) * TP / 2; ++t)
+      for (int t = 0; t < TP / 2; ++t)
 #pragma unroll
-          for (int u = 0; u < TQ; ++u) mma<DT>(a[now][t], b[now][u], acc[t][u]);
-        if (SUMS) {
+        for (int u = 0; u < TQ; ++u) mma<DT>(a[half][t], b[s & 1][u], acc[half * TP / 2 + t][u]);
+      if (SUMS) {
 #pragma unroll
-          for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) add_elements(b[now][u], sums[u]);
-        }
-        // reads and products take turns
-        constexpr int kReads = TP / 2 * (P_COLUMNS ? 16 / kPieceReads : 1) + TQ / 2 * (Q_COLUMNS ? 16 / kPieceReads : 1);
-        constexpr int kTurns = TP / 2 * TQ;
-        constexpr int kProducts = kTurns * (std::is_same<DT, BF16>::value ? 1 : 4);
-        static_for<kTurns>([&](auto i) {
-          constexpr int n = decltype(i)::value;
-          __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / kTurns - kReads * n / kTurns, 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / kTurns - kProducts * n / kTurns, 0);
-        });
-        __builtin_amdgcn_sched_barrier(0);
-        // one load, in the shadow of the products just started
-        if (s == 3 && half == 0) next_q();
-        if (s == 3) Q.load(half, to_q + slot_q * OpQ::kBytes);
-        if (s == 0 && !FIRST) Q.load(2 + half, to_q + (slot_q ^ 1) * OpQ::kBytes);
-        if (s == 1 && half == 0) next_p();
-        if (s == 1 || s == 2) P.load(2 * (s - 1) + half, to_p + slot_free * OpP::kBytes);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int u = half * TQ / 2; u < (half + 1) * TQ / 2; ++u) add_elements(b[s & 1][u], sums[u]);
+      }
+      // reads and products take turns
+      constexpr int kReads = TP / 2 * (P_COLUMNS ? 16 / kPieceReads : 1) + (kLastQ - kFirstQ) * (Q_COLUMNS ? 16 / kPieceReads : 1);
+      constexpr int kTurns = TP / 2 * TQ;
+      constexpr int kProducts = kTurns * (std::is_same<DT, BF16>::value ? 1 : 4);
+      static_for<kTurns>([&](auto jc) {
+        constexpr int n = decltype(jc)::value;
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads * (n + 1) / kTurns - kReads * n / kTurns, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kProducts * (n + 1) / kTurns - kProducts * n / kTurns, 0);
       });
+      __builtin_amdgcn_sched_barrier(0);
+      // one load, in the shadow of the products just started
+      if (kEnd) {
+        next_q();
+        Q.load(0, to_q + slot_q * OpQ::kBytes);
+        if (LAST) {
+#pragma unroll
+          for (int j = 1; j < 4; ++j) Q.load(j, to_q + slot_q * OpQ::kBytes);
+        }
+      } else if (i < 3) {
+        if (!FIRST) Q.load(1 + i, to_q + (slot_q ^ 1) * OpQ::kBytes);
+      } else {
+        if (i == 3) next_p();
+        P.load(i - 3, to_p + slot_free * OpP::kBytes);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     });
-    if (LAST) {
-      Q.load(2, to_q + slot_q * OpQ::kBytes);
-      Q.load(3, to_q + slot_q * OpQ::kBytes);
-    }
     slot_p = slot_next;
     slot_q ^= 1;
   }
@@ -369,7 +372,7 @@ template <typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, i
     for (;;) {
       // the first fragments (again behind a finished tile: they would take registers that its results need)
 #pragma unroll
-      for (int t = 0; t < TP; ++t) a[0][t] = fp.read(base + slot_p * OpP::kBytes, 0, t);
+      for (int t = 0; t < TP / 2; ++t) a[0][t] = fp.read(base + slot_p * OpP::kBytes, 0, t);
 #pragma unroll
       for (int u = 0; u < TQ; ++u) b[0][u] = fq.read(base + kAtQ + slot_q * OpQ::kBytes, 0, u);
 #pragma unroll
