@@ -13,6 +13,7 @@ constexpr int kWave = 64;
 
 struct F32 {};   // IEEE binary32 storage
 struct BF16 {};  // bfloat16 storage (upper half of binary32)
+struct MX4 {};   // 4-bit numbers in blocks with a scale, two to a byte
 
 // Two binary32 -> two bfloat16, round to nearest even; NaN stays NaN.  One instruction (v_cvt_pk_bf16_f32): rounding with
 // integer operations took six per element, in kernels that move rows a third of their vector work.
@@ -111,5 +112,6 @@ template <> struct Piece<BF16> {
 template <typename DT> struct ItemSize;
 template <> struct ItemSize<F32> { static constexpr int value = 4; };
 template <> struct ItemSize<BF16> { static constexpr int value = 2; };
+template <> struct ItemSize<MX4> { static constexpr int value = 1; };   // a byte, two numbers
 
 }  // namespace lshmoe

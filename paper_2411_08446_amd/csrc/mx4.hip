@@ -6,14 +6,13 @@
 // The matrix instruction with scales takes exactly that: a lane's 16 bytes are one block of one row, its scale one byte, so
 // rows go from memory to the matrix cores without a change of layout.
 #include "kernels.h"
-#include "rows_by_expert.h"
+#include "product_tile.h"
 
 namespace lshmoe {
 
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 32;   // numbers that share a scale
 
@@ -115,7 +114,7 @@ __device__ __forceinline__ void load_block(const char* codes, const uint8_t* sca
 
 // out = act(x W_e^T + b_e) of quantised x and W_e.  A wave has 64 columns of 16 rows; operands come straight from memory.
 template <typename DT>
-__global__ __launch_bounds__(256) void forward_kernel(const char* __restrict__ x_codes, const uint8_t* __restrict__ x_scales,
+__global__ __launch_bounds__(256) void direct_kernel(const char* __restrict__ x_codes, const uint8_t* __restrict__ x_scales,
                                                       const char* __restrict__ w_codes, const uint8_t* __restrict__ w_scales,
                                                       const void* bias, const int32_t* __restrict__ offsets, int64_t rows,
                                                       int d_in, int d_out, int E, int act, void* out) {
@@ -174,17 +173,35 @@ hipError_t launch_mx4_dequantize(const void* codes, const uint8_t* scales, int64
   return hipGetLastError();
 }
 
+namespace {
+
+template <typename DT>
+hipError_t forward_mx4(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
+                       const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E, int act, void* out,
+                       hipStream_t stream) {
+  if (d_in % 128 == 0 && rows >= 64 * (int64_t)E) {
+    typedef Tile<MX4, DT, false, false, 256, 256, 2, 4> TILE;
+    auto kernel = forward_kernel<MX4, DT, TILE, 256, 256>;
+    if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
+    const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, 256) * ((d_out + 255) / 256);
+    kernel<<<blocks_for(tiles, 1), TILE::kThreads, TILE::kLds, stream>>>(
+        (const char*)x_codes, (const char*)w_codes, (const char*)x_scales, (const char*)w_scales, (const char*)bias, offsets,
+        (int)rows, d_in, d_out, E, act, nullptr, (char*)out);
+    return hipGetLastError();
+  }
+  const dim3 grid = grid_of_blocks((uint64_t)most_row_tiles(rows, E, kTile) * ((d_out + kTile - 1) / kTile));
+  direct_kernel<DT><<<grid, 256, 0, stream>>>((const char*)x_codes, x_scales, (const char*)w_codes, w_scales, bias, offsets, rows,
+                                              d_in, d_out, E, act, out);
+  return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_expert_forward_mx4(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
                                      const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
                                      bool bf16, int act, void* out, hipStream_t stream) {
-  const dim3 grid = grid_of_blocks((uint64_t)most_row_tiles(rows, E, kTile) * ((d_out + kTile - 1) / kTile));
-  if (bf16)
-    forward_kernel<BF16><<<grid, 256, 0, stream>>>((const char*)x_codes, x_scales, (const char*)w_codes, w_scales, bias, offsets,
-                                                   rows, d_in, d_out, E, act, out);
-  else
-    forward_kernel<F32><<<grid, 256, 0, stream>>>((const char*)x_codes, x_scales, (const char*)w_codes, w_scales, bias, offsets,
-                                                  rows, d_in, d_out, E, act, out);
-  return hipGetLastError();
+  return bf16 ? forward_mx4<BF16>(x_codes, x_scales, w_codes, w_scales, bias, offsets, rows, d_in, d_out, E, act, out, stream)
+              : forward_mx4<F32>(x_codes, x_scales, w_codes, w_scales, bias, offsets, rows, d_in, d_out, E, act, out, stream);
 }
 
 }  // namespace lshmoe
