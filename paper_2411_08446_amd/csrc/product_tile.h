@@ -313,7 +313,8 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
 
   // One chunk's products, the loads of a chunk ahead, the first fragments of the next chunk.  A half step is the products of half
   // of P's tiles: fragments of P are read half a step ahead, of Q a step ahead.  In front of the last half step is the
-  // chunk's barrier.  Loads go one to a half step: while chunk c is at work, Q's of chunk c + 1 and P's of chunk c + 2; Q's of
+  // chunk's barrier.  Loads go two or one to a half step: while chunk c is at work, Q's of chunk c + 1, which is needed
+  // first, then P's of chunk c + 2 (Q's one to a half step: 4 to 7 % more time); Q's of
   // the next tile's second chunk are started at the end of the last one, in front of the results' stores.  With scales:
   // everything of chunk c + 1, two or three to a half step.
   template <bool SUMS, bool FIRST, bool LAST, typename SwitchP, typename SwitchQ>
@@ -405,9 +406,12 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
         }
       } else {
         if (kLoadQ && i == 0) f.next_q();
-        if (kLoadQ && i < 4) f.Q.load(i, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
-        if (i == 3) f.next_p();
-        if (i >= 3 && i < 7) f.P.load(i - 3, f.to_p + slot_free * OpP::kBytes);
+        if (i == 2) f.next_p();
+        if (kLoadQ && i < 2) {
+          f.Q.load(2 * i, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
+          f.Q.load(2 * i + 1, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
+        }
+        if (i >= 2 && i < 6) f.P.load(i - 2, f.to_p + slot_free * OpP::kBytes);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
