@@ -9,8 +9,8 @@
 // A workgroup computes tiles of BQ x BP outputs, one after the other.  k goes by chunks: 128 bytes of every row of an operand
 // that is contiguous in k ("rows"), as many k of one that is not ("columns").  Chunks go from memory straight into LDS, into
 // rings of three chunks of P and two of Q (160 KB for two workgroups of binary32 or one of bf16), one barrier to a chunk.
-// A wave starts one load per half step, between its products: a chunk's loads all at once fill the address units' queue,
-// and the products behind them wait.  The chunks of all tiles of a workgroup are one stream: while a tile's results are
+// A wave spreads its loads between its products: a chunk's loads all at once fill the address units' queue, and the
+// products behind them wait.  The chunks of all tiles of a workgroup are one stream: while a tile's results are
 // stored, the first chunks of the next are on their way.
 #pragma once
 
@@ -155,33 +155,34 @@ template <typename OT, bool COLUMNS, int B, int WAVES> struct Operand {
   }
 };
 
-// The scales of an operand of 4-bit numbers: 8 bytes of each of B rows to a chunk, in LDS as [index][8].  Rows of whole 4 bytes.
+// The scales of two operands of 4-bit numbers, B indices each: 8 bytes of a row to a chunk, in LDS as two words of [P's index, then
+// Q's].  The first half of the waves load P's, the others Q's.  Rows of whole 4 bytes.
 template <int B, int WAVES> struct ScaleOperand {
-  static constexpr int kBytes = B * 8;
-  static_assert(kBytes == 256 * WAVES, "one load of 4 bytes a lane to a wave");
-  uint32_t offset, ahead, now, cut, away, stride;
-  int left;
+  static constexpr int kBytes = 2 * B * 8;
+  static_assert(kBytes == 512 * WAVES, "two loads of 4 bytes a lane to a wave");
+  uint32_t offset, ahead, now, away, stride;
   i32x4 buffer;
+  bool mine_p;
 
   __device__ __forceinline__ explicit ScaleOperand(uint32_t stride_) : stride(stride_) {
-    const int slot = (int)threadIdx.x;
-    offset = (uint32_t)(slot / 2) * stride + slot % 2 * 4;
+    offset = (uint32_t)((int)threadIdx.x % (32 * WAVES)) * stride;
+    mine_p = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64) < WAVES / 2;
   }
-  __device__ __forceinline__ void start(const char* first, int indices, int K) {
-    left = indices == 0 ? 0 : (int)stride;
-    buffer = buffer_of(first, indices == 0 || K == 0 ? 0 : (int64_t)indices * stride);
+  __device__ __forceinline__ void start(const char* first_p, const char* first_q, int np, int nq, int K) {
+    const int n = K == 0 ? 0 : mine_p ? np : nq;
+    buffer = buffer_of(mine_p ? first_p : first_q, (int64_t)n * stride);
     ahead = 0;
-    cut = (int)threadIdx.x % 2 * 4 >= left % 8 ? kNowhere : 0u;
     asm volatile("s_nop 4" : "+s"(buffer));
   }
   __device__ __forceinline__ void next() {
     now = ahead;
     ahead += 8;
-    away = left < 8 ? cut : 0u;
-    left -= 8;
+    away = ahead > stride ? kNowhere : 0u;      // half a chunk: the second word is behind the row's end
     asm volatile("s_nop 4" : "+s"(buffer), "+s"(now));
   }
-  __device__ __forceinline__ void load(uint32_t lds) const { load4_to_lds(buffer, offset | away, now, lds); }
+  __device__ __forceinline__ void load(int i, uint32_t lds) const {
+    load4_to_lds(buffer, i == 0 ? offset : offset + 4 | away, now, lds + i * 256 * WAVES);
+  }
 };
 
 typedef __attribute__((address_space(3))) char lds_char;
@@ -245,17 +246,15 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   static constexpr bool kScaled = std::is_same<OT, MX4>::value;
   static constexpr int kRingP = kScaled ? 2 : 3, kRingQ = 2;
   static constexpr int kAtQ = kRingP * OpP::kBytes, kAtScales = kAtQ + kRingQ * OpQ::kBytes;
-  typedef ScaleOperand<kScaled ? BP : 32 * kWaves, kWaves> ScP;
-  typedef ScaleOperand<kScaled ? BQ : 32 * kWaves, kWaves> ScQ;
-  static constexpr int kScaleBytes = ScP::kBytes + ScQ::kBytes;
-  static constexpr size_t kLds = kAtScales + (kScaled ? 2 * kScaleBytes : 0);
+  static_assert(!kScaled || BP == BQ, "the waves share the scales' loads evenly");
+  typedef ScaleOperand<32 * kWaves, kWaves> Scales;
+  static constexpr size_t kLds = kAtScales + (kScaled ? 2 * Scales::kBytes : 0);
   static_assert(OpP::kLoads == 4 && OpQ::kLoads == 4 && kSteps == 4 && TP % 2 == 0, "a load to a half step");
 
   struct Feed {
     OpP P;
     OpQ Q;
-    ScP SP;
-    ScQ SQ;
+    Scales S;
     lds_char* lds;
     uint32_t to_p, to_q, to_s;   // where a wave's loads go
     int slot_p, slot_q;          // ring slots of the chunk at work
@@ -264,12 +263,11 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     // The next chunk's loads begin.
     __device__ __forceinline__ void next_p() {
       P.next();
-      if constexpr (kScaled) SP.next();
+      if constexpr (kScaled) S.next();
       --chunks_p;
     }
     __device__ __forceinline__ void next_q() {
       Q.next();
-      if constexpr (kScaled) SQ.next();
       --chunks_q;
     }
   };
@@ -290,31 +288,24 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   typedef Fragments<OT, P_COLUMNS, BP, TP> FragP;
   typedef Fragments<OT, Q_COLUMNS, BQ, TQ> FragQ;
 
-  // The chunk's scales from a slot.
-  __device__ __forceinline__ void read_scales(const Feed& f, int slot, u32x2 (&p)[TP], u32x2 (&q)[TQ]) const {
-    typedef __attribute__((address_space(3))) const u32x2* pair;
-    const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-    lds_char* const at = f.lds + kAtScales + slot * kScaleBytes;
-#pragma unroll
-    for (int t = 0; t < TP; ++t) p[t] = *(pair)(at + ((wave % WP * TP + t) * 32 + lane % 32) * 8);
-#pragma unroll
-    for (int u = 0; u < TQ; ++u) q[u] = *(pair)(at + ScP::kBytes + ((wave / WP * TQ + u) * 32 + lane % 32) * 8);
-  }
-  __device__ __forceinline__ void take_scales(const u32x2 (&p)[TP], const u32x2 (&q)[TQ]) {
-    const int shift = (int)threadIdx.x % 64 / 32 * 8;
+  // The scales of the chunk at work.
+  __device__ __forceinline__ void read_scales(const Feed& f) {
+    typedef __attribute__((address_space(3))) const uint32_t* word;
+    const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), shift = lane / 32 * 8;
+    lds_char* const at = f.lds + kAtScales + f.slot_q * Scales::kBytes + lane % 32 * 4;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int t = 0; t < TP; ++t) scale_p[t][i] = p[t][i] >> shift;
+      for (int t = 0; t < TP; ++t) scale_p[t][i] = *(word)(at + i * Scales::kBytes / 2 + (wave % WP * TP + t) * 128) >> shift;
 #pragma unroll
-      for (int u = 0; u < TQ; ++u) scale_q[u][i] = q[u][i] >> shift;
+      for (int u = 0; u < TQ; ++u) scale_q[u][i] = *(word)(at + i * Scales::kBytes / 2 + BP * 4 + (wave / WP * TQ + u) * 128) >> shift;
     }
   }
 
   // One chunk's products, the loads of a chunk ahead, the first fragments of the next chunk.  A half step is the products of half
   // of P's tiles: fragments of P are read half a step ahead, of Q a step ahead.  In front of the last half step is the
-  // chunk's barrier.  Loads go two or one to a half step: while chunk c is at work, Q's of chunk c + 1, which is needed
-  // first, then P's of chunk c + 2 (Q's one to a half step: 4 to 7 % more time); Q's of
+  // chunk's barrier.  While chunk c is at work, Q's loads of chunk c + 1, which is needed first, are started behind the first
+  // half step's products, P's of chunk c + 2 one by one behind the next ones' (Q's one by one too: 6 to 9 % more time); Q's of
   // the next tile's second chunk are started at the end of the last one, in front of the results' stores.  With scales:
   // everything of chunk c + 1, two or three to a half step.
   template <bool SUMS, bool FIRST, bool LAST, typename SwitchP, typename SwitchQ>
@@ -329,15 +320,11 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     // everything that branches is in front of the products: they are one straight line
     if (kLoadQ) switch_q();
     if (kLoadP) switch_p();
-    if constexpr (kScaled) {
-      u32x2 p[TP], q[TQ];
-      read_scales(f, f.slot_q, p, q);
-      take_scales(p, q);
-    }
+    if constexpr (kScaled) read_scales(f);
     auto load_scales = [&](int slot) {
       if constexpr (kScaled) {
-        f.SP.load(f.to_s + slot * kScaleBytes);
-        f.SQ.load(f.to_s + slot * kScaleBytes + ScP::kBytes);
+        f.S.load(0, f.to_s + slot * Scales::kBytes);
+        f.S.load(1, f.to_s + slot * Scales::kBytes);
       }
     };
     static_for<2 * kSteps>([&](auto ic) {
@@ -370,10 +357,13 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
 #pragma unroll
         for (int u = 0; u < TQ; ++u) {
           constexpr int t0 = half * TP / 2;
-          if constexpr (kScaled)
+          if constexpr (kScaled) {
             mma_scaled<s>(a[half][t], b[s & 1][u], scale_p[t0 + t][s / 2], scale_q[u][s / 2], acc[t0 + t][u]);
-          else
+            // the compiler may move this instruction behind later branches, which keeps all fragments alive until there
+            asm volatile("" : "+v"(acc[t0 + t][u]));
+          } else {
             mma<OT>(a[half][t], b[s & 1][u], acc[t0 + t][u]);
+          }
         }
       if constexpr (SUMS) {
 #pragma unroll
@@ -407,11 +397,14 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
       } else {
         if (kLoadQ && i == 0) f.next_q();
         if (i == 2) f.next_p();
-        if (kLoadQ && i < 2) {
-          f.Q.load(2 * i, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
-          f.Q.load(2 * i + 1, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
-        }
-        if (i >= 2 && i < 6) f.P.load(i - 2, f.to_p + slot_free * OpP::kBytes);
+        if (kLoadQ && i == 0) f.Q.load(0, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
+        if (kLoadQ && i == 0) f.Q.load(1, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
+        if (kLoadQ && i == 0) f.Q.load(2, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
+        if (kLoadQ && i == 0) f.Q.load(3, f.to_q + (f.slot_q ^ 1) * OpQ::kBytes);
+        if (i == 2) f.P.load(0, f.to_p + slot_free * OpP::kBytes);
+        if (i == 3) f.P.load(1, f.to_p + slot_free * OpP::kBytes);
+        if (i == 4) f.P.load(2, f.to_p + slot_free * OpP::kBytes);
+        if (i == 5) f.P.load(3, f.to_p + slot_free * OpP::kBytes);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -455,7 +448,7 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const FragP fp(wave % WP * TP * 32);
     const FragQ fq(wave / WP * TQ * 32);
-    Feed f = {OpP(job.p_stride()), OpQ(job.q_stride()), ScP(job.s_stride()), ScQ(job.s_stride()), (lds_char*)lds, 0, 0, 0, 0, 0, 0, 0};
+    Feed f = {OpP(job.p_stride()), OpQ(job.q_stride()), Scales(job.s_stride()), (lds_char*)lds, 0, 0, 0, 0, 0, 0, 0};
     f.to_p = (uint32_t)(uintptr_t)f.lds + wave * 1024;
     f.to_q = f.to_p + kAtQ;
     f.to_s = (uint32_t)(uintptr_t)f.lds + kAtScales + wave * 256;
@@ -476,12 +469,11 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     int at_p = 0, at_q = 0;                                // the tiles that P's and Q's loads are at
     auto start_p = [&](const typename JOB::Place& x) {
       f.P.start(x.p, x.np, x.K);
-      if constexpr (kScaled) f.SP.start(x.scale_p(), x.np, x.K);
+      if constexpr (kScaled) f.S.start(x.w_scales, x.x_scales, x.np, x.nq, x.K);
       f.chunks_p = x.chunks();
     };
     auto start_q = [&](const typename JOB::Place& x) {
       f.Q.start(x.q, x.nq, x.K);
-      if constexpr (kScaled) f.SQ.start(x.scale_q(), x.nq, x.K);
       f.chunks_q = x.chunks();
     };
     auto switch_p = [&] {
@@ -497,19 +489,21 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
       f.next_q();
 #pragma unroll
       for (int i = 0; i < 4; ++i) f.Q.load(i, f.to_q + slot * OpQ::kBytes);
-      if constexpr (kScaled) f.SQ.load(f.to_s + slot * kScaleBytes + ScP::kBytes);
     };
     auto load_p = [&](int slot) {
       switch_p();
       f.next_p();
 #pragma unroll
       for (int i = 0; i < 4; ++i) f.P.load(i, f.to_p + slot * OpP::kBytes);
-      if constexpr (kScaled) f.SP.load(f.to_s + slot * kScaleBytes);
+      if constexpr (kScaled) {
+        f.S.load(0, f.to_s + slot * Scales::kBytes);
+        f.S.load(1, f.to_s + slot * Scales::kBytes);
+      }
     };
     load_q(0);
     load_p(0);
     load_p(1);
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kScaled ? 5 : 4) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kScaled ? 6 : 4) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
     load_q(1);
@@ -699,8 +693,6 @@ __device__ __forceinline__ Share share_of_block(int total) {
 struct PlaceOfRows {
   const char *p, *q, *w_scales, *x_scales;
   int np, nq, K, chunk, expert, first, p0;
-  __device__ __forceinline__ const char* scale_p() const { return w_scales; }
-  __device__ __forceinline__ const char* scale_q() const { return x_scales; }
   __device__ __forceinline__ int chunks() const { return max((K + chunk - 1) / chunk, 1); }
   __device__ __forceinline__ static PlaceOfRows none(const PlaceOfRows& like) {
     PlaceOfRows x = like;
@@ -764,7 +756,7 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
     }
   }
   template <int ACT> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
-    if (pre) store<ACT, true>(at, tile);
+    if (!kScaled && pre) store<ACT, !kScaled>(at, tile);
     else store<ACT, false>(at, tile);
   }
   __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
