@@ -8,6 +8,7 @@
 //
 // The tiles and how they are computed: product_tile.h.
 #include "kernels.h"
+#include "product_direct.h"
 #include "product_tile.h"
 
 namespace lshmoe {
@@ -42,7 +43,7 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
     const typename TILE::Lines k = TILE::lines((ACT == LSHMOE_ACT_NONE ? grad_x : pre) + first, (uint32_t)d_in * kItem, at.nq, at.np);
     // The values before the activation come in two halves, both loaded before anything is stored, as in the forward product; the
     // first half's results wait, packed.
-    constexpr int kHalf = TILE::kGroups / 2;
+    constexpr int kHalf = TILE::kGroups > 1 ? TILE::kGroups / 2 : 1;
     typename TILE::Pieces x[kHalf][TILE::TQ], y[kHalf][TILE::TQ];
     auto get = [&](int g0) {
 #pragma unroll
@@ -76,10 +77,14 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
     };
     if (ACT != LSHMOE_ACT_NONE) get(0);
     scale(0);
-    if (ACT != LSHMOE_ACT_NONE) get(kHalf);
-    put(0);
-    scale(kHalf);
-    put(kHalf);
+    if constexpr (TILE::kGroups > 1) {
+      if (ACT != LSHMOE_ACT_NONE) get(kHalf);
+      put(0);
+      scale(kHalf);
+      put(kHalf);
+    } else {
+      put(0);
+    }
   }
   __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
     if (act == LSHMOE_ACT_RELU) store<LSHMOE_ACT_RELU>(at, tile);
@@ -174,10 +179,9 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const ch
   tile.run(job, s.first, s.end, s.step);
 }
 
-template <typename DT>
-hipError_t forward(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out,
-                   int E, int act, void* pre, void* out, hipStream_t stream) {
-  typedef Shape<DT> S;
+template <typename DT, typename S>
+hipError_t forward_on_tiles(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows, int d_in,
+                            int d_out, int E, int act, void* pre, void* out, hipStream_t stream) {
   typedef Tile<DT, DT, false, false, S::BP, S::BQ, S::WP, S::WQ> TILE;
   auto kernel = forward_kernel<DT, DT, TILE, S::BP, S::BQ>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
@@ -188,10 +192,26 @@ hipError_t forward(const void* x, const void* w, const void* bias, const int32_t
   return hipGetLastError();
 }
 
+// Rows per expert that a call can have at most on average decide.  Up to 8 (binary32: 32): waves that read the weights for
+// themselves (768 -> 2048 columns of 16 experts: 74 rows 13.1 and 13.9 us on tiles, 2048 -> 768 13.1 and 22.9; 256 rows 15.6
+// and 13.8; binary32, 512 rows 38.6 and 57, 1024 rows 61.5 and 56).  Up to 128: small tiles (1024 -> 4096 columns of 16
+// experts, 2048 rows 28.7 us and 34 on large ones, 4096 rows 43.3 and 39.5).
 template <typename DT>
-hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
-                      int act, const void* pre, void* grad_x, hipStream_t stream) {
-  typedef Shape<DT> S;
+hipError_t forward(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out,
+                   int E, int act, void* pre, void* out, hipStream_t stream) {
+  constexpr bool kWide = std::is_same<DT, F32>::value;
+  if (rows <= (kWide ? 32 : 8) * (int64_t)E)
+    return launch_direct<DT, DT>((const char*)x, (const char*)w, nullptr, nullptr, (const char*)bias, offsets, rows,
+                                 d_in * ItemSize<DT>::value, d_out, E, act, (char*)pre, (char*)out, stream);
+  if constexpr (!kWide)
+    if (rows > 128 * (int64_t)E)
+      return forward_on_tiles<DT, Large>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out, stream);
+  return forward_on_tiles<DT, Small>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out, stream);
+}
+
+template <typename DT, typename S>
+hipError_t input_grad_on_tiles(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in, int d_out,
+                               int E, int act, const void* pre, void* grad_x, hipStream_t stream) {
   typedef Tile<DT, DT, true, false, S::BP, S::BQ, S::WP, S::WQ> TILE;
   auto kernel = input_grad_kernel<DT, TILE, S::BP, S::BQ>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
@@ -202,9 +222,18 @@ hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offset
 }
 
 template <typename DT>
+hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
+                      int act, const void* pre, void* grad_x, hipStream_t stream) {
+  if constexpr (!std::is_same<DT, F32>::value)
+    if (rows > 128 * (int64_t)E)
+      return input_grad_on_tiles<DT, Large>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
+  return input_grad_on_tiles<DT, Small>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
+}
+
+template <typename DT>
 hipError_t weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
                        void* grad_w, void* grad_bias, hipStream_t stream) {
-  typedef Shape<DT> S;
+  typedef typename std::conditional<std::is_same<DT, F32>::value, Small, Large>::type S;
   typedef Tile<DT, DT, true, true, S::BP, S::BQ, S::WP, S::WQ> TILE;
   auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;

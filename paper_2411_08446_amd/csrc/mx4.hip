@@ -6,13 +6,12 @@
 // The matrix instruction with scales takes exactly that: a lane's 16 bytes are one block of one row, its scale one byte, so
 // rows go from memory to the matrix cores without a change of layout.
 #include "kernels.h"
+#include "product_direct.h"
 #include "product_tile.h"
 
 namespace lshmoe {
 
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlock = 32;   // numbers that share a scale
 
@@ -91,65 +90,6 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const char* __restrict_
   }
 }
 
-constexpr int kTile = 64;   // outputs of a workgroup in either direction
-
-template <typename DT> __device__ __forceinline__ float widen_at(const void* p, int64_t i);
-template <> __device__ __forceinline__ float widen_at<F32>(const void* p, int64_t i) { return ((const float*)p)[i]; }
-template <> __device__ __forceinline__ float widen_at<BF16>(const void* p, int64_t i) { return (float)((const __bf16*)p)[i]; }
-template <typename DT> __device__ __forceinline__ void store_at(void* p, int64_t i, float v);
-template <> __device__ __forceinline__ void store_at<F32>(void* p, int64_t i, float v) { ((float*)p)[i] = v; }
-template <> __device__ __forceinline__ void store_at<BF16>(void* p, int64_t i, float v) { ((__bf16*)p)[i] = (__bf16)v; }
-
-// 16 bytes of codes and the scale byte of block `block` of a row; a block behind the row's end is zeros.
-__device__ __forceinline__ void load_block(const char* codes, const uint8_t* scales, int64_t row, int blocks, int block,
-                                           i32x8& v, int& scale) {
-  uint4 q = make_uint4(0u, 0u, 0u, 0u);
-  scale = 127;
-  if (block < blocks) {
-    q = load16(codes + (row * blocks + block) * 16);
-    scale = scales[row * blocks + block];
-  }
-  v = (i32x8){(int)q.x, (int)q.y, (int)q.z, (int)q.w, 0, 0, 0, 0};
-}
-
-// out = act(x W_e^T + b_e) of quantised x and W_e.  A wave has 64 columns of 16 rows; operands come straight from memory.
-template <typename DT>
-__global__ __launch_bounds__(256) void direct_kernel(const char* __restrict__ x_codes, const uint8_t* __restrict__ x_scales,
-                                                      const char* __restrict__ w_codes, const uint8_t* __restrict__ w_scales,
-                                                      const void* bias, const int32_t* __restrict__ offsets, int64_t rows,
-                                                      int d_in, int d_out, int E, int act, void* out) {
-  const int ptiles = (d_out + kTile - 1) / kTile;
-  const RowTiles tiles(offsets, E, (int)rows, kTile);
-  if (linear_block() >= (uint64_t)tiles.total * ptiles) return;
-  const RowTile t = tiles.find((int)linear_block(), ptiles);
-  const int p0 = t.column * kTile;
-  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, r = lane % 16, g = lane / 16;
-  const int blocks = d_in / kBlock;
-  const int64_t q = (int64_t)t.first + 16 * wave + r, end = (int64_t)t.first + t.rows;
-  f32x4 acc[4] = {};
-  for (int k = 0; k < blocks; k += 4) {
-    i32x8 b, a;
-    int sb, sa;
-    load_block(x_codes, x_scales, min(q, end - 1), blocks, k + g, b, sb);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      load_block(w_codes, w_scales, (int64_t)t.expert * d_out + min(p0 + 16 * i + r, d_out - 1), blocks, k + g, a, sa);
-      acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[i], 4, 4, 0, sa, 0, sb);
-    }
-  }
-  if (q >= end) return;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int p = p0 + 16 * i + 4 * g + j;
-      if (p >= d_out) continue;
-      float v = acc[i][j];
-      if (bias) v += widen_at<DT>(bias, (int64_t)t.expert * d_out + p);
-      store_at<DT>(out, q * d_out + p, activate(v, act));
-    }
-}
-
 }  // namespace
 
 hipError_t launch_mx4_quantize(const void* x, int64_t rows, int d, bool bf16, void* codes, uint8_t* scales, hipStream_t stream) {
@@ -175,11 +115,15 @@ hipError_t launch_mx4_dequantize(const void* codes, const uint8_t* scales, int64
 
 namespace {
 
+// Up to so many rows per expert the waves that read the weights for themselves are faster than the tiles (768 -> 2048 columns of
+// 16 experts, 32 rows to each: 11.2 and 16.3 us; 64 rows: 18.9 and 13.9).  Tiles move scales by 4 bytes.
+constexpr int kFewRows = 32;
+
 template <typename DT>
 hipError_t forward_mx4(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
                        const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E, int act, void* out,
                        hipStream_t stream) {
-  if (d_in % 128 == 0 && rows >= 64 * (int64_t)E) {
+  if (d_in % 128 == 0 && rows > kFewRows * (int64_t)E) {
     typedef Tile<MX4, DT, false, false, 256, 256, 2, 4> TILE;
     auto kernel = forward_kernel<MX4, DT, TILE, 256, 256>;
     if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
@@ -189,10 +133,8 @@ hipError_t forward_mx4(const void* x_codes, const uint8_t* x_scales, const void*
         (int)rows, d_in, d_out, E, act, nullptr, (char*)out);
     return hipGetLastError();
   }
-  const dim3 grid = grid_of_blocks((uint64_t)most_row_tiles(rows, E, kTile) * ((d_out + kTile - 1) / kTile));
-  direct_kernel<DT><<<grid, 256, 0, stream>>>((const char*)x_codes, x_scales, (const char*)w_codes, w_scales, bias, offsets, rows,
-                                              d_in, d_out, E, act, out);
-  return hipGetLastError();
+  return launch_direct<MX4, DT>((const char*)x_codes, (const char*)w_codes, (const char*)x_scales, (const char*)w_scales,
+                                (const char*)bias, offsets, rows, d_in / 2, d_out, E, act, nullptr, (char*)out, stream);
 }
 
 }  // namespace

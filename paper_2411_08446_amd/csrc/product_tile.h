@@ -782,8 +782,9 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void forward_kernel(const char* 
   tile.run(job, s.first, s.end, s.step);
 }
 
-template <typename DT> struct Shape { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, kPerUnit = 1; };
-template <> struct Shape<F32> { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, kPerUnit = 2; };
+// Tiles: 256 x 256 by 8 waves, one workgroup to a compute unit, or 128 x 128 by 4 waves, two of them (binary32 always).
+struct Large { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, kPerUnit = 1; };
+struct Small { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, kPerUnit = 2; };
 
 // More than 64 KB of LDS has to be asked for, once per kernel and device; asking again is harmless.
 template <typename K> hipError_t allow_lds(K kernel, size_t bytes) {
