@@ -133,7 +133,7 @@ lshmoe_status lshmoe_expert_workspace_bytes(int64_t rows, int32_t d_in, int32_t 
                                             size_t* out_bytes) {
   if (!out_bytes) return fail(LSHMOE_ERR_NULL, "out_bytes is NULL");
   if (lshmoe_status st = check_product(rows, d_in, d_out, E, (int)dtype)) return st;
-  *out_bytes = lshmoe::expert_workspace_bytes(rows, d_in, d_out, E, dtype == LSHMOE_BF16);
+  *out_bytes = lshmoe::expert_workspace_bytes(rows, d_in, d_out, dtype == LSHMOE_BF16);
   return ok();
 }
 
@@ -144,7 +144,7 @@ lshmoe_status lshmoe_expert_backward_weight(const void* grad_out, const void* x,
     return fail(LSHMOE_ERR_NULL, "grad_out, x, expert_offsets and grad_w must be non-NULL");
   if (lshmoe_status st = check_product(rows, d_in, d_out, E, (int)dtype)) return st;
   if (lshmoe_status st = check_aligned({grad_out, x, expert_offsets, grad_w, grad_bias})) return st;
-  const size_t need = lshmoe::expert_workspace_bytes(rows, d_in, d_out, E, dtype == LSHMOE_BF16);
+  const size_t need = lshmoe::expert_workspace_bytes(rows, d_in, d_out, dtype == LSHMOE_BF16);
   if (need > 0) {
     if (!workspace) return fail(LSHMOE_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
     if (((uintptr_t)workspace & 255u) != 0) return fail(LSHMOE_ERR_WORKSPACE, "workspace is not 256-byte aligned");

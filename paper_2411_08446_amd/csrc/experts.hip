@@ -27,9 +27,9 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
   __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
   __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_out * kItem; }
   __device__ __forceinline__ uint32_t s_stride() const { return 0; }
-  __device__ __forceinline__ TileEntry entry(int n) const {
-    const RowTile t = tiles.find(n, ptiles);
-    return {{t.expert, t.first, t.rows, t.column * BP}};
+  template <bool AGAIN> __device__ __forceinline__ TileEntry entry(int n) const {
+    const RowTile t = tiles.template tile<AGAIN>(n, ptiles);
+    return {{t.expert, t.first, t.rows, t.column * BP, 0}};
   }
   __device__ __forceinline__ Place place(const TileEntry& t) const {
     const int expert = t.v[0], first = t.v[1], nq = t.v[2], p0 = t.v[3];
@@ -107,10 +107,27 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void input_grad_kernel(const cha
   tile.run(job, s.first, s.end, s.step);
 }
 
+// Rows of a part of an expert's rows (see RowParts): a workgroup's share of the work.  Parts below 512 rows are not worth their
+// partial sums' way through memory.
+constexpr int kLeastPart = 512;
+__host__ __device__ inline int part_rows(int64_t rows, int64_t tiles, int workgroups) {
+  const int64_t share = rows * tiles / workgroups;
+  return (int)(share > kLeastPart ? share : kLeastPart);
+}
+// Partial sums are kept at the number of their first row over half a part: parts of experts that are cut begin further apart.
+inline uint64_t part_slots(int64_t rows, int64_t tiles, int workgroups) {
+  // a share rounded down twice, of 256 rows at least: less than 1 / 64 more slots
+  const uint64_t fine = 2 * (uint64_t)workgroups / (uint64_t)tiles, most = fine + fine / 64 + 2;
+  const uint64_t all = (uint64_t)rows / (kLeastPart / 2) + 1;
+  return most < all ? most : all;
+}
+
+// Gradients of W_e and b_e.  An expert with many rows is cut into parts; a part's sums go to the workspace in binary32, in the
+// order in which the lanes hold them, and a second kernel adds the parts up, first to last.
 template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
   struct Place {
     const char *p, *q;
-    int np, nq, K, expert, p0, q0;
+    int np, nq, K, expert, p0, q0, tile, slot;    // slot: of the partial sums, or -1: the expert is one part
     __device__ __forceinline__ int chunks() const { return max((K + TILE::OpP::kChunk - 1) / TILE::OpP::kChunk, 1); }
     __device__ __forceinline__ static Place none(const Place& like) {
       Place x = like;
@@ -122,26 +139,76 @@ template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
   static constexpr int kItem = ItemSize<DT>::value;
   const char *grad_out, *x;
   char *grad_w, *grad_bias;
-  const int32_t* offsets;
-  int rows, d_in, d_out, E, ptiles, qtiles;
+  float4* partial;        // [slot][tile][TP TQ 4][thread]
+  float* partial_sums;    // [slot][tile][TQ][thread]
+  int d_in, d_out, ptiles, qtiles, slots;
+  const RowParts& parts;
 
   __device__ __forceinline__ uint32_t p_stride() const { return (uint32_t)d_in * kItem; }
   __device__ __forceinline__ uint32_t q_stride() const { return (uint32_t)d_out * kItem; }
   __device__ __forceinline__ uint32_t s_stride() const { return 0; }
-  __device__ __forceinline__ TileEntry entry(int n) const {
-    const int e = min((int)((uint32_t)n / (uint32_t)(ptiles * qtiles)), E - 1);
-    const RowRange range = rows_of(offsets, e, rows);
-    return {{e, n - e * ptiles * qtiles, range.lo, range.hi - range.lo}};
+  // (the bound is for offsets that are no offsets)
+  __device__ __forceinline__ int slot_of(int first_row) const {
+    return min((int)((uint32_t)first_row / (uint32_t)(parts.pieces.goal / 2)), slots - 1);
+  }
+  template <bool AGAIN> __device__ __forceinline__ TileEntry entry(int n) const {
+    const int m = (int)((uint32_t)n / (uint32_t)(ptiles * qtiles));
+    return entry_of(parts.template find<AGAIN>(m), n - m * ptiles * qtiles);
+  }
+  __device__ __forceinline__ TileEntry entry_of(const RowParts::Found& f, int tile) const {
+    const int first = part_start(f.range, f.count, f.number), end = part_start(f.range, f.count, f.number + 1);
+    return {{f.expert, tile, first, end - first, f.count > 1 ? slot_of(first) : -1}};
   }
   __device__ __forceinline__ Place place(const TileEntry& t) const {
     const int e = t.v[0], q = (int)((uint32_t)t.v[1] / (uint32_t)ptiles), p0 = (t.v[1] - q * ptiles) * BP, q0 = q * BQ;
     return {x + ((int64_t)t.v[2] * d_in + p0) * kItem, grad_out + ((int64_t)t.v[2] * d_out + q0) * kItem, min(BP, d_in - p0),
-            min(BQ, d_out - q0), t.v[3], e, p0, q0};
+            min(BQ, d_out - q0), t.v[3], e, p0, q0, t.v[1], t.v[4]};
   }
   __device__ __forceinline__ bool sums(const Place& at) const { return grad_bias != nullptr && at.p0 == 0; }
+  __device__ __forceinline__ float4* partial_at(int slot, int tile, int i, int thread) const {
+    return partial + (((int64_t)slot * ptiles * qtiles + tile) * (TILE::TP * TILE::TQ * 4) + i) * TILE::kThreads + thread;
+  }
+  __device__ __forceinline__ float* sums_at(int slot, int tile, int u, int thread) const {
+    return partial_sums + (((int64_t)slot * ptiles * qtiles + tile) * TILE::TQ + u) * TILE::kThreads + thread;
+  }
+
   __device__ __forceinline__ void finish(const Place& at, const TILE& tile) const {
-    const typename TILE::Lines o = TILE::lines(grad_w + (((int64_t)at.expert * d_out + at.q0) * d_in + at.p0) * kItem,
-                                               (uint32_t)d_in * kItem, at.nq, at.np);
+    if (at.slot < 0) {
+      store(at, tile);
+      return;
+    }
+#pragma unroll
+    for (int t = 0; t < TILE::TP; ++t)
+#pragma unroll
+      for (int u = 0; u < TILE::TQ; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *partial_at(at.slot, at.tile, (t * TILE::TQ + u) * 4 + j, (int)threadIdx.x) =
+              make_float4(tile.acc[t][u][4 * j], tile.acc[t][u][4 * j + 1], tile.acc[t][u][4 * j + 2], tile.acc[t][u][4 * j + 3]);
+    if (sums(at))
+#pragma unroll
+      for (int u = 0; u < TILE::TQ; ++u) *sums_at(at.slot, at.tile, u, (int)threadIdx.x) = tile.sums[u];
+  }
+
+  __device__ __forceinline__ typename TILE::Lines lines(const Place& at, int wave) const {
+    return TILE::lines(grad_w + (((int64_t)at.expert * d_out + at.q0) * d_in + at.p0) * kItem, (uint32_t)d_in * kItem, at.nq, at.np,
+                       wave);
+  }
+  // The sums over Q of tile u of a wave: the waves of one column of waves have the same, the first stores them, the lane
+  // halves' joined.
+  __device__ __forceinline__ void store_sums(const Place& at, int wave, int u, float half) const {
+    constexpr int kWP = BP / 32 / TILE::TP;
+    const int lane = (int)threadIdx.x % 64, q = (wave / kWP * TILE::TQ + u) * 32 + lane;
+    const float sum = half + __shfl_xor(half, 32, 64);
+    if (wave % kWP != 0 || lane >= 32 || q >= at.nq) return;
+    const int64_t i = (int64_t)at.expert * d_out + at.q0 + q;
+    if (kItem == 4) reinterpret_cast<float*>(grad_bias)[i] = sum;
+    else reinterpret_cast<__bf16*>(grad_bias)[i] = (__bf16)sum;
+  }
+
+  __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const typename TILE::Lines o = lines(at, wave);
 #pragma unroll
     for (int g = 0; g < TILE::kGroups; ++g)
 #pragma unroll
@@ -151,32 +218,93 @@ template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
         TILE::put(o, g, u, TILE::pack(v));
       }
     if (!sums(at)) return;
-    // the waves of one column of waves have the same Q: the first stores, the lane halves' sums joined
-    constexpr int kWP = BP / 32 / TILE::TP;
-    const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
 #pragma unroll
-    for (int u = 0; u < TILE::TQ; ++u) {
-      const float sum = tile.sums[u] + __shfl_xor(tile.sums[u], 32, 64);
-      const int q = (wave / kWP * TILE::TQ + u) * 32 + lane;
-      if (wave % kWP != 0 || lane >= 32 || q >= at.nq) continue;
-      const int64_t i = (int64_t)at.expert * d_out + at.q0 + q;
-      if (kItem == 4) reinterpret_cast<float*>(grad_bias)[i] = sum;
-      else reinterpret_cast<__bf16*>(grad_bias)[i] = (__bf16)sum;
+    for (int u = 0; u < TILE::TQ; ++u) store_sums(at, wave, u, tile.sums[u]);
+  }
+
+  // Adds up and stores group g, tile u of what wave `wave` of a tile's workgroup had of each part.
+  __device__ __forceinline__ void join(const Place& at, const RowRange& range, int count, int wave, int g, int u) const {
+    constexpr int kElems = 16 * TILE::kGroupTiles;
+    const int thread = wave * 64 + (int)threadIdx.x % 64;
+    const bool with_sums = sums(at) && g == 0;
+    float v[kElems] = {}, sum = 0.0f;
+#pragma unroll 2
+    for (int k = 0; k < count; ++k) {
+      const int slot = slot_of(part_start(range, count, k));
+#pragma unroll
+      for (int i = 0; i < kElems / 4; ++i) {
+        const int t = g * TILE::kGroupTiles + i / 4;
+        const float4 x = *partial_at(slot, at.tile, (t * TILE::TQ + u) * 4 + i % 4, thread);
+        v[4 * i] += x.x;
+        v[4 * i + 1] += x.y;
+        v[4 * i + 2] += x.z;
+        v[4 * i + 3] += x.w;
+      }
+      if (with_sums) sum += *sums_at(slot, at.tile, u, thread);
     }
+    typename TILE::Lines o = lines(at, wave);
+    // u and g are no constants here: the first group and tile of lines moved on to them
+    o.at += (uint32_t)u * 32 * o.ld + 128u * g;
+    o.p += 32 * TILE::kGroupTiles * g;
+    TILE::put(o, 0, 0, TILE::pack(v));
+    if (with_sums) store_sums(at, wave, u, sum);
   }
 };
 
-template <typename DT, typename TILE, int BP, int BQ>
+template <typename DT, typename TILE, int BP, int BQ, int PER_UNIT>
 __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const char* __restrict__ grad_out,
                                                                         const char* __restrict__ x,
                                                                         const int32_t* __restrict__ offsets, int rows, int d_in,
                                                                         int d_out, int E, char* __restrict__ grad_w,
-                                                                        char* __restrict__ grad_bias) {
+                                                                        char* __restrict__ grad_bias, float4* partial,
+                                                                        float* partial_sums, int slots) {
   const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ;
-  const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, offsets, rows, d_in, d_out, E, ptiles, qtiles};
-  const Share s = share_of_block(E * ptiles * qtiles);
+  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, ptiles * qtiles, kUnits * PER_UNIT));
+  const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, partial, partial_sums, d_in, d_out, ptiles, qtiles,
+                                               slots, parts};
+  // an XCD's tiles are consecutive ones with an eighth of the work
+  const RowRange mine = parts.run_of_work((int)(blockIdx.x % 8), 8, ptiles * qtiles);
   TILE tile;
-  tile.run(job, s.first, s.end, s.step);
+  tile.run(job, mine.lo + (int)(blockIdx.x / 8), mine.hi, (int)(gridDim.x / 8));
+}
+
+// Adds up the parts of the experts that were cut: a wave takes a group's results of one wave of a tile's workgroup.  It looks at 64
+// of them at a time; most calls have none that were cut.
+constexpr int kJoinThreads = 256;
+template <typename DT, typename TILE, int BP, int BQ, int PER_UNIT>
+__global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(const int32_t* __restrict__ offsets, int rows, int d_in,
+                                                                  int d_out, int E, char* __restrict__ grad_w,
+                                                                  char* __restrict__ grad_bias, float4* partial,
+                                                                  float* partial_sums, int slots) {
+  const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ, tiles = ptiles * qtiles;
+  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, tiles, kUnits * PER_UNIT));
+  if (parts.total == E) return;            // no expert was cut
+  const WeightGradJob<DT, TILE, BP, BQ> job = {nullptr, nullptr, grad_w, grad_bias, partial, partial_sums, d_in, d_out, ptiles,
+                                               qtiles, slots, parts};
+  constexpr int kShares = TILE::kWaves * TILE::kGroups * TILE::TQ;     // of a tile
+  // Number i is share i % kShares of tile i / kShares; a wave's lanes look at the tiles of 64 numbers, its own ones.
+  const int lane = (int)threadIdx.x % kWave;
+  const int64_t waves = (int64_t)gridDim.x * (kJoinThreads / kWave), all = (int64_t)parts.total * tiles * kShares;
+  const int64_t self = (int64_t)blockIdx.x * (kJoinThreads / kWave) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  for (int64_t i0 = self; i0 < all; i0 += waves * kWave) {
+    const int64_t i = min(i0 + lane * waves, all - 1);
+    const int n = (int)(i / kShares);
+    const int m = (int)((uint32_t)n / (uint32_t)tiles);
+    const RowParts::Found f = parts.find(m);
+    const TileEntry entry = job.entry_of(f, n - m * tiles);
+    uint64_t cut = __ballot(f.count > 1 && f.number == 0 && i0 + lane * waves < all);
+    while (cut != 0) {
+      const int at = __builtin_ctzll(cut);
+      cut &= cut - 1;
+      TileEntry e;
+#pragma unroll
+      for (int j = 0; j < 5; ++j) e.v[j] = __builtin_amdgcn_readlane(entry.v[j], at);
+      const RowRange range = {__builtin_amdgcn_readlane(f.range.lo, at), __builtin_amdgcn_readlane(f.range.hi, at)};
+      const int share = (int)((i0 + at * waves) % kShares);
+      job.join(job.place(e), range, __builtin_amdgcn_readlane(f.count, at), share % TILE::kWaves, share / TILE::kWaves % TILE::kGroups,
+               share / TILE::kWaves / TILE::kGroups);
+    }
+  }
 }
 
 template <typename DT, typename S>
@@ -230,16 +358,42 @@ hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offset
   return input_grad_on_tiles<DT, Small>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
 }
 
+template <typename DT> struct WeightGradShape : Large {};
+template <> struct WeightGradShape<F32> : Small {};
+
+template <typename DT> struct WeightGradPlan {
+  typedef WeightGradShape<DT> S;
+  typedef Tile<DT, DT, true, true, S::BP, S::BQ, S::WP, S::WQ> TILE;
+  uint64_t tiles;         // of an expert
+  bool cut;               // there may be experts in parts
+  uint64_t slots;         // of partial sums
+  size_t off_sums, total_bytes;
+
+  WeightGradPlan(int64_t rows, int d_in, int d_out) {
+    tiles = (uint64_t)((d_in + S::BP - 1) / S::BP) * ((d_out + S::BQ - 1) / S::BQ);
+    cut = rows > kLeastPart;
+    slots = cut ? part_slots(rows, tiles, kUnits * S::kPerUnit) : 0;
+    off_sums = slots * tiles * S::BP * S::BQ * 4;
+    total_bytes = off_sums + slots * tiles * TILE::TQ * TILE::kThreads * 4;
+  }
+};
+
 template <typename DT>
 hipError_t weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
-                       void* grad_w, void* grad_bias, hipStream_t stream) {
-  typedef typename std::conditional<std::is_same<DT, F32>::value, Small, Large>::type S;
-  typedef Tile<DT, DT, true, true, S::BP, S::BQ, S::WP, S::WQ> TILE;
-  auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ>;
+                       void* grad_w, void* grad_bias, char* workspace, hipStream_t stream) {
+  typedef WeightGradShape<DT> S;
+  typedef typename WeightGradPlan<DT>::TILE TILE;
+  const WeightGradPlan<DT> plan(rows, d_in, d_out);
+  auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ, S::kPerUnit>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
-  const uint64_t tiles = (uint64_t)E * ((d_in + S::BP - 1) / S::BP) * ((d_out + S::BQ - 1) / S::BQ);
-  kernel<<<blocks_for(tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
-      (const char*)grad_out, (const char*)x, offsets, (int)rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias);
+  float4* const partial = (float4*)workspace;
+  float* const sums = (float*)(workspace + plan.off_sums);
+  const uint64_t parts = (uint64_t)E + (plan.cut ? rows / (kLeastPart / 2) : 0);
+  kernel<<<blocks_for(parts * plan.tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)grad_out, (const char*)x, offsets, (int)rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias, partial, sums, (int)plan.slots);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !plan.cut) return e;
+  join_parts_kernel<DT, TILE, S::BP, S::BQ, S::kPerUnit><<<2 * kUnits, kJoinThreads, 0, stream>>>(
+      offsets, (int)rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias, partial, sums, (int)plan.slots);
   return hipGetLastError();
 }
 
@@ -257,12 +411,15 @@ hipError_t launch_expert_input_grad(const void* grad_out, const void* w, const i
               : input_grad<F32>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
 }
 
-size_t expert_workspace_bytes(int64_t, int, int, int, bool) { return 0; }
+size_t expert_workspace_bytes(int64_t rows, int d_in, int d_out, bool bf16) {
+  return bf16 ? WeightGradPlan<BF16>(rows, d_in, d_out).total_bytes : WeightGradPlan<F32>(rows, d_in, d_out).total_bytes;
+}
 
 hipError_t launch_expert_weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in,
-                                     int d_out, int E, bool bf16, void* grad_w, void* grad_bias, char*, hipStream_t stream) {
-  return bf16 ? weight_grad<BF16>(grad_out, x, offsets, rows, d_in, d_out, E, grad_w, grad_bias, stream)
-              : weight_grad<F32>(grad_out, x, offsets, rows, d_in, d_out, E, grad_w, grad_bias, stream);
+                                     int d_out, int E, bool bf16, void* grad_w, void* grad_bias, char* workspace,
+                                     hipStream_t stream) {
+  return bf16 ? weight_grad<BF16>(grad_out, x, offsets, rows, d_in, d_out, E, grad_w, grad_bias, workspace, stream)
+              : weight_grad<F32>(grad_out, x, offsets, rows, d_in, d_out, E, grad_w, grad_bias, workspace, stream);
 }
 
 }  // namespace lshmoe

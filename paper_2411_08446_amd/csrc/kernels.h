@@ -109,7 +109,7 @@ hipError_t launch_expert_forward(const void* x, const void* w, const void* bias,
                                  int d_in, int d_out, int E, bool bf16, int act, void* pre, void* out, hipStream_t stream);
 hipError_t launch_expert_input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in,
                                     int d_out, int E, bool bf16, int act, const void* pre, void* grad_x, hipStream_t stream);
-size_t expert_workspace_bytes(int64_t rows, int d_in, int d_out, int E, bool bf16);
+size_t expert_workspace_bytes(int64_t rows, int d_in, int d_out, bool bf16);
 hipError_t launch_expert_weight_grad(const void* grad_out, const void* x, const int32_t* offsets, int64_t rows, int d_in,
                                      int d_out, int E, bool bf16, void* grad_w, void* grad_bias, char* workspace,
                                      hipStream_t stream);

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void direct_kernel(const char* __restrict__ x,
   const RowTiles tiles(offsets, E, rows, 16 * TQ);
   const int ptiles = (d_out + turns * kColumns - 1) / (turns * kColumns);
   if (linear_block() >= (uint64_t)tiles.total * ptiles) return;
-  const RowTile t = tiles.find((int)linear_block(), ptiles);
+  const RowTile t = tiles.tile((int)linear_block(), ptiles);
   const int expert = __builtin_amdgcn_readfirstlane(t.expert), first = __builtin_amdgcn_readfirstlane(t.first);
   const int nq = __builtin_amdgcn_readfirstlane(t.rows);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), part = wave % KS;

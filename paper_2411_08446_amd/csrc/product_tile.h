@@ -233,7 +233,7 @@ template <typename OT, bool COLUMNS, int B, int T> struct Fragments {
   }
 };
 
-struct TileEntry { int v[4]; };
+struct TileEntry { int v[5]; };
 
 // OT: type of the operands, DT: of the results.
 template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int BQ, int WP, int WQ> struct Tile {
@@ -454,15 +454,15 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     f.to_s = (uint32_t)(uintptr_t)f.lds + kAtScales + wave * 256;
     const int count = (end - n + step - 1) / step;       // tiles
     int at = 0, table_at = 0;                              // the tile at work, the first of the table's
-    TileEntry table = job.entry(n + (int)(threadIdx.x % kWave) * step);
+    TileEntry table = job.template entry<false>(n + (int)(threadIdx.x % kWave) * step);
     auto place = [&](int i) {
       if (i - table_at >= kWave) {
         table_at = at;
-        table = job.entry(n + (at + (int)(threadIdx.x % kWave)) * step);
+        table = job.template entry<true>(n + (at + (int)(threadIdx.x % kWave)) * step);
       }
       TileEntry e;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) e.v[j] = __builtin_amdgcn_readlane(table.v[j], i - table_at);
+      for (int j = 0; j < 5; ++j) e.v[j] = __builtin_amdgcn_readlane(table.v[j], i - table_at);
       return job.place(e);
     };
     typename JOB::Place here = place(0);
@@ -545,7 +545,10 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   };
   // first: the tile's first element in an array of lines of ld bytes; nq by np of it exist.
   __device__ __forceinline__ static Lines lines(const char* first, uint32_t ld, int nq, int np) {
-    const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    return lines(first, ld, nq, np, __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64));
+  }
+  __device__ __forceinline__ static Lines lines(const char* first, uint32_t ld, int nq, int np, int wave) {
+    const int lane = (int)threadIdx.x % 64;
     const int64_t bytes = nq == 0 ? 0 : (int64_t)(nq - 1) * ld + np * ItemSize<DT>::value;
     Lines l;
     l.buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
@@ -716,9 +719,9 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
   __device__ __forceinline__ uint32_t p_stride() const { return line(); }
   __device__ __forceinline__ uint32_t q_stride() const { return line(); }
   __device__ __forceinline__ uint32_t s_stride() const { return d_in / 32; }
-  __device__ __forceinline__ TileEntry entry(int n) const {
-    const RowTile t = tiles.find(n, ptiles);
-    return {{t.expert, t.first, t.rows, t.column * BP}};
+  template <bool AGAIN> __device__ __forceinline__ TileEntry entry(int n) const {
+    const RowTile t = tiles.template tile<AGAIN>(n, ptiles);
+    return {{t.expert, t.first, t.rows, t.column * BP, 0}};
   }
   __device__ __forceinline__ Place place(const TileEntry& t) const {
     const int expert = t.v[0], first = t.v[1], nq = t.v[2], p0 = t.v[3];

@@ -28,21 +28,37 @@ struct RowTile {
   int column;           // its tile of columns
 };
 
-// The experts' row tiles of `tile` rows, in the order of the experts.  Every wave counts them by itself: lane e % 64 has expert
-// e's, summed over the lanes, 64 experts at a time.
-struct RowTiles {
+// Things of the experts (row tiles, parts of their rows), numbered in the order of the experts; pieces(n) says how many an expert
+// of n rows has.  Every wave counts them by itself: lane e % 64 has expert e's, summed over the lanes, 64 experts at a time.
+template <typename PIECES> struct ByExpert {
   const int32_t* offsets;
-  int rows, E, tile;
+  int rows, E;
+  PIECES pieces;
   int total;
+  RowRange range0;        // what count(0, ..) gives
+  int mine0, upto0;
 
-  // Of expert e0 + lane: its rows, the tiles of experts e0 up to and with it.
-  __device__ __forceinline__ void count(int e0, int& lo, int& hi, int& upto) const {
+  // Of expert e0 + lane: its rows, how many it has, how many experts e0 up to and with it have.  AGAIN: not from what is kept, which
+  // would stay in registers until then.
+  template <bool AGAIN = false>
+  __device__ __forceinline__ void count(int e0, RowRange& range, int& mine, int& upto) const {
+    if (!AGAIN && e0 == 0) {
+      range = range0;
+      mine = mine0;
+      upto = upto0;
+    } else {
+      look(e0, range, mine, upto);
+    }
+  }
+  __device__ __forceinline__ void look(int e0, RowRange& range, int& mine, int& upto) const {
     const int lane = (int)threadIdx.x % kWave;
-    RowRange range = {0, 0};
-    if (e0 + lane < E) range = rows_of(offsets, e0 + lane, rows);
-    lo = range.lo;
-    hi = range.hi;
-    upto = (hi - lo + tile - 1) / tile;
+    range = {0, 0};
+    mine = 0;
+    if (e0 + lane < E) {
+      range = rows_of(offsets, e0 + lane, rows);
+      mine = pieces(range.hi - range.lo);
+    }
+    upto = mine;
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) {
       const int below = __shfl_up(upto, s, kWave);
@@ -50,48 +66,120 @@ struct RowTiles {
     }
   }
 
-  __device__ __forceinline__ RowTiles(const int32_t* __restrict__ offsets_, int E_, int rows_, int tile_)
-      : offsets(offsets_), rows(rows_), E(E_), tile(tile_), total(0) {
-    for (int e0 = 0; e0 < E; e0 += kWave) {
-      int lo, hi, upto;
-      count(e0, lo, hi, upto);
+  __device__ __forceinline__ ByExpert(const int32_t* __restrict__ offsets_, int E_, int rows_, const PIECES& pieces_)
+      : offsets(offsets_), rows(rows_), E(E_), pieces(pieces_), total(0) {
+    look(0, range0, mine0, upto0);
+    total = __builtin_amdgcn_readlane(upto0, kWave - 1);
+    for (int e0 = kWave; e0 < E; e0 += kWave) {
+      RowRange range;
+      int mine, upto;
+      count(e0, range, mine, upto);
       total += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
   }
 
-  // Tile n of the experts' row tiles by `columns` tiles of columns; every lane may ask for another one, and all lanes of a wave
-  // ask together (n >= total * columns gives anything).  An expert's tiles go in bands of kBand row tiles, within a band
-  // column after column: the tiles that run at a time on an XCD are about as many rows as columns wide and share what
-  // they read (bands of 8: 3 % less time than bands of 4, 6 % less than
-  // row by row at 4096 -> 4096 columns).
-  __device__ __forceinline__ RowTile find(int n, int columns) const {
-    constexpr int kBand = 8;
-    const int m = (int)((uint32_t)n / (uint32_t)columns);
-    int before = 0;                           // tiles of the experts below e0
-    RowTile t = {0, 0, 0, 0};
+  struct Found {
+    int expert;
+    RowRange range;
+    int count, number;    // how many its expert has, which of them it is
+  };
+  // Number m; every lane may ask for another one, and all lanes of a wave ask together (m >= total gives expert 0 with
+  // nothing).
+  template <bool AGAIN = false> __device__ __forceinline__ Found find(int m) const {
+    int before = 0;                           // of the experts below e0
+    Found f = {0, {0, 0}, 0, 0};
     for (int e0 = 0; e0 < E; e0 += kWave) {
-      int lo, hi, upto;
-      count(e0, lo, hi, upto);
+      RowRange range;
+      int mine, upto;
+      count<AGAIN>(e0, range, mine, upto);
       const int here = __builtin_amdgcn_readlane(upto, kWave - 1);
-      int at = 0;                             // experts of these 64 that end at or before tile m
+      int at = 0;                             // experts of these 64 that end at or before m
 #pragma unroll
       for (int s = kWave / 2; s >= 1; s >>= 1)
         if (before + __shfl(upto, at + s - 1, kWave) <= m) at += s;
       at = min(at, kWave - 1);
-      const int rlo = __shfl(lo, at, kWave), rhi = __shfl(hi, at, kWave), past = __shfl(upto, at, kWave);
-      if (m >= before && m < before + here) {
-        const int mine = (rhi - rlo + tile - 1) / tile;
-        const int inside = n - (before + past - mine) * columns;          // its number in the expert
-        const int band = (int)((uint32_t)inside / (uint32_t)(kBand * columns)), rest = inside - band * kBand * columns;
-        const int wide = min(kBand, mine - band * kBand);
-        t.expert = e0 + at;
-        t.column = (int)((uint32_t)rest / (uint32_t)wide);
-        t.first = rlo + (band * kBand + rest - t.column * wide) * tile;
-        t.rows = min(tile, rhi - t.first);
-      }
+      const RowRange there = {__shfl(range.lo, at, kWave), __shfl(range.hi, at, kWave)};
+      const int past = __shfl(upto, at, kWave), its = __shfl(mine, at, kWave);
+      if (m >= before && m < before + here) f = {e0 + at, there, its, m - (before + past - its)};
       before += here;
     }
+    return f;
+  }
+};
+
+struct TilePieces {
+  int tile;
+  __device__ __forceinline__ int operator()(int n) const { return (n + tile - 1) / tile; }
+};
+
+// The experts' row tiles of `tile` rows.
+struct RowTiles : ByExpert<TilePieces> {
+  __device__ __forceinline__ RowTiles(const int32_t* __restrict__ offsets_, int E_, int rows_, int tile_)
+      : ByExpert(offsets_, E_, rows_, TilePieces{tile_}) {}
+
+  // Tile n of the experts' row tiles by `columns` tiles of columns; lanes as above.  An expert's tiles go in bands of kBand row
+  // tiles, within a band column after column: the tiles that run at a time on an XCD are about as many rows as columns
+  // wide and share what they read (bands of 8: 3 % less time than bands of 4, 6 % less than row by row at 4096 -> 4096
+  // columns).
+  template <bool AGAIN = false> __device__ __forceinline__ RowTile tile(int n, int columns) const {
+    constexpr int kBand = 8;
+    const int m = (int)((uint32_t)n / (uint32_t)columns);
+    const Found f = find<AGAIN>(m);
+    const int inside = f.number * columns + (n - m * columns);            // its number in the expert
+    const int band = (int)((uint32_t)inside / (uint32_t)(kBand * columns)), rest = inside - band * kBand * columns;
+    const int wide = max(min(kBand, f.count - band * kBand), 1);
+    RowTile t;
+    t.expert = f.expert;
+    t.column = (int)((uint32_t)rest / (uint32_t)wide);
+    t.first = f.range.lo + (band * kBand + rest - t.column * wide) * pieces.tile;
+    t.rows = min(pieces.tile, f.range.hi - t.first);
     return t;
+  }
+};
+
+// Parts of at most `goal` rows and a twentieth for the sums over an expert's rows; an expert without rows is one part.  Part k of
+// `count` of n rows begins at k n / count, the next one more than goal / 2 rows behind it.
+struct RowPieces {
+  int goal;
+  __device__ __forceinline__ int operator()(int n) const {
+    return max((int)((uint32_t)(n + (goal - goal / 64 * 3)) / (uint32_t)goal), 1);
+  }
+};
+__device__ __forceinline__ int part_start(const RowRange& range, int count, int k) {
+  return range.lo + (int)((int64_t)(range.hi - range.lo) * k / max(count, 1));
+}
+
+struct RowParts : ByExpert<RowPieces> {
+  __device__ __forceinline__ RowParts(const int32_t* __restrict__ offsets_, int E_, int rows_, int goal)
+      : ByExpert(offsets_, E_, rows_, RowPieces{goal}) {}
+
+  // All parts' tiles, `tiles` to a part, in `of` runs of about the same work: where run x begins and ends.  A tile's work is its rows
+  // and kOver more for what does not depend on them.
+  __device__ __forceinline__ RowRange run_of_work(int x, int of, int tiles) const {
+    constexpr int kOver = 256;
+    const int64_t whole = (int64_t)rows_of(offsets, E - 1, rows).hi + (int64_t)kOver * total;
+    int before = 0, n[2] = {0, 0};
+    for (int e0 = 0; e0 < E; e0 += kWave) {
+      RowRange range;
+      int mine, upto;
+      count(e0, range, mine, upto);
+      const int64_t start = range.lo + (int64_t)kOver * (before + upto - mine);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t goal = whole * (x + i) / of;
+        const uint64_t begun = __ballot(mine > 0 && start <= goal);
+        if (begun == 0) continue;
+        const int at = kWave - 1 - __builtin_clzll(begun);        // the last expert that begins at or before the goal
+        const RowRange r = {__builtin_amdgcn_readlane(range.lo, at), __builtin_amdgcn_readlane(range.hi, at)};
+        const int its = __builtin_amdgcn_readlane(mine, at), first = before + __builtin_amdgcn_readlane(upto, at) - its;
+        const int64_t into = goal - (r.lo + (int64_t)kOver * first), each = (r.hi - r.lo) / its + kOver;
+        const int k = (int)min(into / each, (int64_t)its - 1);
+        n[i] = (first + k) * tiles + (int)min((into - k * each) * tiles / each, (int64_t)tiles);
+      }
+      before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    const int all = total * tiles;
+    return {x == 0 ? 0 : min(n[0], all), x + 1 == of ? all : min(n[1], all)};
   }
 };
 
