@@ -107,20 +107,25 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void input_grad_kernel(const cha
   tile.run(job, s.first, s.end, s.step);
 }
 
-// Rows of a part of an expert's rows (see RowParts): a workgroup's share of the work.  Parts below 512 rows are not worth their
-// partial sums' way through memory.
+// Rows of a part of an expert's rows (see RowParts): a workgroup's share of the work, in binary32 a quarter of that (its products
+// take 16 times as long as bf16's, the partial sums' way through memory does not: 576 tiles on 512 workgroups, 15011 rows,
+// 1000 -> 1500 columns, 466 -> 402 us).  Parts below 512 rows are not worth that way.
 constexpr int kLeastPart = 512;
-__host__ __device__ inline int part_rows(int64_t rows, int64_t tiles, int workgroups) {
-  const int64_t share = rows * tiles / workgroups;
+__host__ __device__ inline int part_rows(int64_t rows, int64_t tiles, int parts) {
+  const int64_t share = rows * tiles / parts;
   return (int)(share > kLeastPart ? share : kLeastPart);
 }
 // Partial sums are kept at the number of their first row over half a part: parts of experts that are cut begin further apart.
-inline uint64_t part_slots(int64_t rows, int64_t tiles, int workgroups) {
+inline uint64_t part_slots(int64_t rows, int64_t tiles, int parts) {
   // a share rounded down twice, of 256 rows at least: less than 1 / 64 more slots
-  const uint64_t fine = 2 * (uint64_t)workgroups / (uint64_t)tiles, most = fine + fine / 64 + 2;
+  const uint64_t fine = 2 * (uint64_t)parts / (uint64_t)tiles, most = fine + fine / 64 + 2;
   const uint64_t all = (uint64_t)rows / (kLeastPart / 2) + 1;
   return most < all ? most : all;
 }
+
+// PARTS: tiles' parts that all workgroups together should have.
+template <typename DT> struct WeightGradShape : Large { static constexpr int PARTS = kUnits * kPerUnit; };
+template <> struct WeightGradShape<F32> : Small { static constexpr int PARTS = 4 * kUnits * kPerUnit; };
 
 // Gradients of W_e and b_e.  An expert with many rows is cut into parts; a part's sums go to the workspace in binary32, in the
 // order in which the lanes hold them, and a second kernel adds the parts up, first to last.
@@ -251,7 +256,7 @@ template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
   }
 };
 
-template <typename DT, typename TILE, int BP, int BQ, int PER_UNIT>
+template <typename DT, typename TILE, int BP, int BQ, int PARTS>
 __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const char* __restrict__ grad_out,
                                                                         const char* __restrict__ x,
                                                                         const int32_t* __restrict__ offsets, int rows, int d_in,
@@ -259,7 +264,7 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const ch
                                                                         char* __restrict__ grad_bias, float4* partial,
                                                                         float* partial_sums, int slots) {
   const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ;
-  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, ptiles * qtiles, kUnits * PER_UNIT));
+  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, ptiles * qtiles, PARTS));
   const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, partial, partial_sums, d_in, d_out, ptiles, qtiles,
                                                slots, parts};
   // an XCD's tiles are consecutive ones with an eighth of the work
@@ -271,13 +276,13 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const ch
 // Adds up the parts of the experts that were cut: a wave takes a group's results of one wave of a tile's workgroup.  It looks at 64
 // of them at a time; most calls have none that were cut.
 constexpr int kJoinThreads = 256;
-template <typename DT, typename TILE, int BP, int BQ, int PER_UNIT>
+template <typename DT, typename TILE, int BP, int BQ, int PARTS>
 __global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(const int32_t* __restrict__ offsets, int rows, int d_in,
                                                                   int d_out, int E, char* __restrict__ grad_w,
                                                                   char* __restrict__ grad_bias, float4* partial,
                                                                   float* partial_sums, int slots) {
   const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ, tiles = ptiles * qtiles;
-  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, tiles, kUnits * PER_UNIT));
+  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, tiles, PARTS));
   if (parts.total == E) return;            // no expert was cut
   const WeightGradJob<DT, TILE, BP, BQ> job = {nullptr, nullptr, grad_w, grad_bias, partial, partial_sums, d_in, d_out, ptiles,
                                                qtiles, slots, parts};
@@ -358,8 +363,6 @@ hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offset
   return input_grad_on_tiles<DT, Small>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
 }
 
-template <typename DT> struct WeightGradShape : Large {};
-template <> struct WeightGradShape<F32> : Small {};
 
 template <typename DT> struct WeightGradPlan {
   typedef WeightGradShape<DT> S;
@@ -372,7 +375,7 @@ template <typename DT> struct WeightGradPlan {
   WeightGradPlan(int64_t rows, int d_in, int d_out) {
     tiles = (uint64_t)((d_in + S::BP - 1) / S::BP) * ((d_out + S::BQ - 1) / S::BQ);
     cut = rows > kLeastPart;
-    slots = cut ? part_slots(rows, tiles, kUnits * S::kPerUnit) : 0;
+    slots = cut ? part_slots(rows, tiles, S::PARTS) : 0;
     off_sums = slots * tiles * S::BP * S::BQ * 4;
     total_bytes = off_sums + slots * tiles * TILE::TQ * TILE::kThreads * 4;
   }
@@ -384,7 +387,7 @@ hipError_t weight_grad(const void* grad_out, const void* x, const int32_t* offse
   typedef WeightGradShape<DT> S;
   typedef typename WeightGradPlan<DT>::TILE TILE;
   const WeightGradPlan<DT> plan(rows, d_in, d_out);
-  auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ, S::kPerUnit>;
+  auto kernel = weight_grad_kernel<DT, TILE, S::BP, S::BQ, S::PARTS>;
   if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
   float4* const partial = (float4*)workspace;
   float* const sums = (float*)(workspace + plan.off_sums);
@@ -392,7 +395,7 @@ hipError_t weight_grad(const void* grad_out, const void* x, const int32_t* offse
   kernel<<<blocks_for(parts * plan.tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
       (const char*)grad_out, (const char*)x, offsets, (int)rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias, partial, sums, (int)plan.slots);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !plan.cut) return e;
-  join_parts_kernel<DT, TILE, S::BP, S::BQ, S::kPerUnit><<<2 * kUnits, kJoinThreads, 0, stream>>>(
+  join_parts_kernel<DT, TILE, S::BP, S::BQ, S::PARTS><<<2 * kUnits, kJoinThreads, 0, stream>>>(
       offsets, (int)rows, d_in, d_out, E, (char*)grad_w, (char*)grad_bias, partial, sums, (int)plan.slots);
   return hipGetLastError();
 }

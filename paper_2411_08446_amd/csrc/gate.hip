@@ -1,10 +1,12 @@
 // Router: the k experts of a token from the logits of its gate, with their weights, and the gradient of the logits.
 //
-// G lanes share a token (G a power of two, E / 4 rounded up); lane i of them holds the logits 4 (i + G c) + j, so that a
-// token's row comes in whole 16-byte pieces.  Choosing is k rounds of an arg-max over the lanes' own best candidates: the
+// G lanes share a token (G a power of two, up to 16 pieces of 4 logits to a lane, c = 0 .. C - 1); lane i of them holds the logits
+// 4 (i + G c) + j, so that a token's row comes in whole 16-byte pieces.  Choosing is k rounds of an arg-max over the lanes' own best candidates: the
 // comparison is on (value, lower index), so a round's winner does not depend on the order of the exchanges.
 //
 // The bound is the read of the logits (and in the backward pass the write of their gradient): 4 E bytes per token.
+#include <type_traits>
+
 #include "kernels.h"
 
 namespace lshmoe {
@@ -21,15 +23,31 @@ __device__ __forceinline__ uint32_t order_of(float v) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+// The value of a lane of the other half of 2 M lanes, where the M lanes of each half hold the same: lane ^ M, or a lane mirrored in 8
+// or 16, which moves within the vector unit.  Lanes 16 and 32 apart go through LDS's crossbar.
+template <int M> __device__ __forceinline__ uint32_t other_half(uint32_t v) {
+  constexpr int kQuad1 = 0xb1, kQuad2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;   // lanes 1 0 3 2; 2 3 0 1; 7 - i; 15 - i
+  constexpr int kControl = M == 1 ? kQuad1 : M == 2 ? kQuad2 : M == 4 ? kHalfMirror : kMirror;
+  if (M > 8) return (uint32_t)__shfl_xor((int)v, M, 64);
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kControl, 0xf, 0xf, true);
+}
+template <int M> __device__ __forceinline__ float other_half(float v) { return __uint_as_float(other_half<M>(__float_as_uint(v))); }
+
+// f(std::integral_constant<int, M>) for M = 1, 2, .. below G.
+template <int G, int M = 1, typename F> __device__ __forceinline__ void over_halves(F&& f) {
+  if constexpr (M < G) {
+    f(std::integral_constant<int, M>{});
+    over_halves<G, 2 * M>(f);
+  }
+}
+
 template <int G> __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int m = G / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+  over_halves<G>([&](auto m) { v += other_half<decltype(m)::value>(v); });
   return v;
 }
 
 template <int G> __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int m = G / 2; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, 64));
+  over_halves<G>([&](auto m) { v = fmaxf(v, other_half<decltype(m)::value>(v)); });
   return v;
 }
 
@@ -78,17 +96,16 @@ __global__ __launch_bounds__(kGateThreads) void gate_topk_kernel(const float* __
         val = v[i];
       }
     }
-#pragma unroll
-    for (int m = G / 2; m >= 1; m >>= 1) {
-      const uint32_t obest = (uint32_t)__shfl_xor((int)best, m, 64);
-      const int oat = __shfl_xor(at, m, 64);
-      const float oval = __shfl_xor(val, m, 64);
-      if (obest > best || (obest == best && oat < at)) {
+    over_halves<G>([&](auto m) {
+      constexpr int M = decltype(m)::value;
+      const uint32_t obest = other_half<M>(best), oat = other_half<M>((uint32_t)at);
+      const float oval = other_half<M>(val);
+      if (obest > best || (obest == best && (int)oat < at)) {
         best = obest;
-        at = oat;
+        at = (int)oat;
         val = oval;
       }
-    }
+    });
 #pragma unroll
     for (int i = 0; i < 4 * C; ++i)
       if (4 * (lane + G * (i / 4)) + i % 4 == at) left[i] = 0u;
@@ -199,9 +216,9 @@ template <int G, int C> hipError_t launch_backward(const float* logits, const in
   if (E <= 16) return call(4, 1);                  \
   if (E <= 32) return call(8, 1);                  \
   if (E <= 64) return call(16, 1);                 \
-  if (E <= 128) return call(32, 1);                \
-  if (E <= 256) return call(64, 1);                \
-  if (E <= 512) return call(64, 2);                \
+  if (E <= 128) return call(16, 2);                \
+  if (E <= 256) return call(16, 4);                \
+  if (E <= 512) return call(32, 4);                \
   return call(64, 4);
 
 hipError_t launch_gate_topk(const float* logits, int64_t T, int E, int k, bool full, int32_t* expert, float* weight,

@@ -60,33 +60,36 @@ __global__ __launch_bounds__(256) void quantize_kernel(const char* __restrict__ 
   scales[b] = (uint8_t)byte;
 }
 
+// A thread has pieces of 16 bytes of the result, 256 pieces apart: its neighbours' stores are next to its own.  Bound by the
+// stores: 131072 x 1024 bf16 48 us, 7.0 TB/s with the codes (a thread per block, 64 bytes to a lane: 89; stores that stay in the caches: 60).
+constexpr int kReadPieces = 4;
 template <typename DT>
 __global__ __launch_bounds__(256) void dequantize_kernel(const char* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                         char* __restrict__ out, uint64_t blocks) {
+                                                         char* __restrict__ out, uint64_t pieces) {
   constexpr int kElems = Piece<DT>::kElems, kPieces = kBlock / kElems;
-  const uint64_t b = linear_block() * 256 + threadIdx.x;
-  if (b >= blocks) return;
-  const uint4 q = load16(codes + b * 16);
-  const uint32_t word[4] = {q.x, q.y, q.z, q.w}, byte = scales[b];
-  const float scale = scale_value(byte == 255u ? 127u : byte);
-  float v[kBlock];
+  const uint64_t first = linear_block() * (256 * kReadPieces) + threadIdx.x;
+  uint32_t word[kReadPieces], byte[kReadPieces];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 0);
-    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 1);
-    const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 2);
-    const f32x2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 3);
-    v[8 * i] = a[0]; v[8 * i + 1] = a[1]; v[8 * i + 2] = c[0]; v[8 * i + 3] = c[1];
-    v[8 * i + 4] = d[0]; v[8 * i + 5] = d[1]; v[8 * i + 6] = e[0]; v[8 * i + 7] = e[1];
+  for (int i = 0; i < kReadPieces; ++i) {
+    const uint64_t p = first + 256 * i < pieces ? first + 256 * i : pieces - 1;
+    word[i] = kElems == 8 ? *reinterpret_cast<const uint32_t*>(codes + p * 4) : *reinterpret_cast<const uint16_t*>(codes + p * 2);
+    byte[i] = scales[p / kPieces];
   }
 #pragma unroll
-  for (int i = 0; i < kBlock; ++i) v[i] = byte == 255u ? __uint_as_float(0x7fc00000u) : v[i];
+  for (int i = 0; i < kReadPieces; ++i) {
+    const float scale = scale_value(byte[i] == 255u ? 127u : byte[i]);
+    float v[kElems];
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 0);
+    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 1);
+    v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
+    if constexpr (kElems == 8) {
+      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 2);
+      const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 3);
+      v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
+    }
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
-    float e[kElems];
-#pragma unroll
-    for (int j = 0; j < kElems; ++j) e[j] = v[i * kElems + j];
-    store16(out + (b * kPieces + i) * 16, Piece<DT>::narrow(e));
+    for (int j = 0; j < kElems; ++j) v[j] = byte[i] == 255u ? __uint_as_float(0x7fc00000u) : v[j];
+    if (first + 256 * i < pieces) store16_stream(out + (first + 256 * i) * 16, Piece<DT>::narrow(v));
   }
 }
 
@@ -104,12 +107,12 @@ hipError_t launch_mx4_quantize(const void* x, int64_t rows, int d, bool bf16, vo
 
 hipError_t launch_mx4_dequantize(const void* codes, const uint8_t* scales, int64_t rows, int d, bool bf16, void* out,
                                  hipStream_t stream) {
-  const uint64_t blocks = (uint64_t)rows * (d / kBlock);
-  const dim3 grid = grid_of_blocks((blocks + 255) / 256);
+  const uint64_t pieces = (uint64_t)rows * (d / (bf16 ? 8 : 4));
+  const dim3 grid = grid_of_blocks((pieces + 256 * kReadPieces - 1) / (256 * kReadPieces));
   if (bf16)
-    dequantize_kernel<BF16><<<grid, 256, 0, stream>>>((const char*)codes, scales, (char*)out, blocks);
+    dequantize_kernel<BF16><<<grid, 256, 0, stream>>>((const char*)codes, scales, (char*)out, pieces);
   else
-    dequantize_kernel<F32><<<grid, 256, 0, stream>>>((const char*)codes, scales, (char*)out, blocks);
+    dequantize_kernel<F32><<<grid, 256, 0, stream>>>((const char*)codes, scales, (char*)out, pieces);
   return hipGetLastError();
 }
 
