@@ -325,19 +325,17 @@ hipError_t forward_on_tiles(const void* x, const void* w, const void* bias, cons
   return hipGetLastError();
 }
 
-// Rows per expert that a call can have at most on average decide.  Up to 8 (binary32: 32): waves that read the weights for
-// themselves (768 -> 2048 columns of 16 experts: 74 rows 13.1 and 13.9 us on tiles, 2048 -> 768 13.1 and 22.9; 256 rows 15.6
-// and 13.8; binary32, 512 rows 38.6 and 57, 1024 rows 61.5 and 56).  Up to 128: small tiles (1024 -> 4096 columns of 16
-// experts, 2048 rows 28.7 us and 34 on large ones, 4096 rows 43.3 and 39.5).
+// binary32's tiles take 16 times as long: few rows are up to 32 (512 rows, 768 -> 2048 columns of 16 experts 38.6 and 57 us, 1024
+// rows 61.5 and 56).
 template <typename DT>
 hipError_t forward(const void* x, const void* w, const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out,
                    int E, int act, void* pre, void* out, hipStream_t stream) {
   constexpr bool kWide = std::is_same<DT, F32>::value;
-  if (rows <= (kWide ? 32 : 8) * (int64_t)E)
+  if (few_rows(rows, E, d_out, kWide ? 32 : 8))
     return launch_direct<DT, DT>((const char*)x, (const char*)w, nullptr, nullptr, (const char*)bias, offsets, rows,
                                  d_in * ItemSize<DT>::value, d_out, E, act, (char*)pre, (char*)out, stream);
   if constexpr (!kWide)
-    if (rows > 128 * (int64_t)E)
+    if (!small_tiles(rows, E, d_out))
       return forward_on_tiles<DT, Large>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out, stream);
   return forward_on_tiles<DT, Small>(x, w, bias, offsets, rows, d_in, d_out, E, act, pre, out, stream);
 }
@@ -358,7 +356,7 @@ template <typename DT>
 hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E,
                       int act, const void* pre, void* grad_x, hipStream_t stream) {
   if constexpr (!std::is_same<DT, F32>::value)
-    if (rows > 128 * (int64_t)E)
+    if (!small_tiles(rows, E, d_in))
       return input_grad_on_tiles<DT, Large>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
   return input_grad_on_tiles<DT, Small>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
 }

@@ -118,26 +118,31 @@ hipError_t launch_mx4_dequantize(const void* codes, const uint8_t* scales, int64
 
 namespace {
 
-// Up to so many rows per expert the waves that read the weights for themselves are faster than the tiles (768 -> 2048 columns of
-// 16 experts, 32 rows to each: 11.2 and 16.3 us; 64 rows: 18.9 and 13.9).  Tiles move scales by 4 bytes.
-constexpr int kFewRows = 32;
+template <typename DT, typename S>
+hipError_t forward_on_tiles(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
+                            const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E, int act,
+                            void* out, hipStream_t stream) {
+  typedef Tile<MX4, DT, false, false, S::BP, S::BQ, S::WP, S::WQ> TILE;
+  auto kernel = forward_kernel<MX4, DT, TILE, S::BP, S::BQ>;
+  if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
+  const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, S::BQ) * ((d_out + S::BP - 1) / S::BP);
+  kernel<<<blocks_for(tiles, S::kPerUnit), TILE::kThreads, TILE::kLds, stream>>>(
+      (const char*)x_codes, (const char*)w_codes, (const char*)x_scales, (const char*)w_scales, (const char*)bias, offsets,
+      (int)rows, d_in, d_out, E, act, nullptr, (char*)out);
+  return hipGetLastError();
+}
 
+// Tiles move scales by 4 bytes, and so take rows of whole 128 numbers.
 template <typename DT>
 hipError_t forward_mx4(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
                        const void* bias, const int32_t* offsets, int64_t rows, int d_in, int d_out, int E, int act, void* out,
                        hipStream_t stream) {
-  if (d_in % 128 == 0 && rows > kFewRows * (int64_t)E) {
-    typedef Tile<MX4, DT, false, false, 256, 256, 2, 4> TILE;
-    auto kernel = forward_kernel<MX4, DT, TILE, 256, 256>;
-    if (hipError_t e = allow_lds(kernel, TILE::kLds); e != hipSuccess) return e;
-    const uint64_t tiles = (uint64_t)most_row_tiles(rows, E, 256) * ((d_out + 255) / 256);
-    kernel<<<blocks_for(tiles, 1), TILE::kThreads, TILE::kLds, stream>>>(
-        (const char*)x_codes, (const char*)w_codes, (const char*)x_scales, (const char*)w_scales, (const char*)bias, offsets,
-        (int)rows, d_in, d_out, E, act, nullptr, (char*)out);
-    return hipGetLastError();
-  }
-  return launch_direct<MX4, DT>((const char*)x_codes, (const char*)w_codes, (const char*)x_scales, (const char*)w_scales,
-                                (const char*)bias, offsets, rows, d_in / 2, d_out, E, act, nullptr, (char*)out, stream);
+  if (d_in % 128 != 0 || few_rows(rows, E, d_out, 8))
+    return launch_direct<MX4, DT>((const char*)x_codes, (const char*)w_codes, (const char*)x_scales, (const char*)w_scales,
+                                  (const char*)bias, offsets, rows, d_in / 2, d_out, E, act, nullptr, (char*)out, stream);
+  if (small_tiles(rows, E, d_out))
+    return forward_on_tiles<DT, Small>(x_codes, x_scales, w_codes, w_scales, bias, offsets, rows, d_in, d_out, E, act, out, stream);
+  return forward_on_tiles<DT, Large>(x_codes, x_scales, w_codes, w_scales, bias, offsets, rows, d_in, d_out, E, act, out, stream);
 }
 
 }  // namespace

@@ -785,16 +785,32 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void forward_kernel(const char* 
   tile.run(job, s.first, s.end, s.step);
 }
 
+constexpr int kUnits = 256;   // compute units
+
 // Tiles: 256 x 256 by 8 waves, one workgroup to a compute unit, or 128 x 128 by 4 waves, two of them (binary32 always).
 struct Large { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, kPerUnit = 1; };
 struct Small { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, kPerUnit = 2; };
+
+// Small tiles where a call has at most 128 rows per expert on average or fewer large tiles than compute units (1024 -> 4096 columns
+// of 16 experts: 2048 rows 28.7 us and 34 on large tiles, 4096 rows 43.3 and 39.5; 4 bits 16.2 and 19.7, 23.6 and 21.8;
+// 512 -> 512 columns of 8 experts, 16384 rows, 4 bits: 12.0 and 15.2; with work enough large ones are 20 % faster).
+inline bool small_tiles(int64_t rows, int E, int columns) {
+  return rows <= 128 * (int64_t)E || (uint64_t)most_row_tiles(rows, E, Large::BQ) * ((columns + Large::BP - 1) / Large::BP) < (uint64_t)kUnits;
+}
+
+// Waves that read the weights for themselves (product_direct.h) where a call has at most `few` rows per expert on average and no more
+// small tiles than run at a time (16 experts, 74 rows: 768 -> 2048 columns 13.1 and 13.9 us on tiles, 2048 -> 768 13.1 and
+// 22.9; 4 bits 8.9 and 9.3, 9.4 and 11.6; 256 rows 15.6 and 13.8; 64 experts, 256 rows, 1024 -> 4096 columns 100 and 96, 4 bits
+// 47 and 35).
+inline bool few_rows(int64_t rows, int E, int columns, int few) {
+  return rows <= few * (int64_t)E && (uint64_t)most_row_tiles(rows, E, Small::BQ) * ((columns + Small::BP - 1) / Small::BP) <=
+                                         (uint64_t)kUnits * Small::kPerUnit;
+}
 
 // More than 64 KB of LDS has to be asked for, once per kernel and device; asking again is harmless.
 template <typename K> hipError_t allow_lds(K kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
-
-constexpr int kUnits = 256;   // compute units
 
 // Workgroups for at most this many tiles: as many as run at a time, a multiple of the 8 XCDs.
 inline uint32_t blocks_for(uint64_t tiles, int per_unit) {
