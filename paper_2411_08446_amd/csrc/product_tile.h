@@ -60,15 +60,15 @@ template <int S> __device__ __forceinline__ void mma_scaled(const u32x4& a, cons
 
 // 16 bytes per lane from a buffer straight into LDS: lane l's piece, offset + ahead bytes into the buffer, lands at dst + 16 l (ahead
 // and dst are wave-uniform); a lane whose piece is behind the buffer's end gets zeros.  Inline assembly, because behind the compiler's own builtin every LDS read
-// waits until the load has landed; the caller waits for these loads itself.
+// waits until the load has landed; the caller waits for these loads itself.  Between m0's write and its use is one wait state.
 __device__ __forceinline__ void load16_to_lds(const i32x4& buffer, uint32_t offset, uint32_t ahead, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds"
                : : "v"(offset), "s"(dst), "s"(buffer), "s"(ahead) : "memory", "m0");
 }
 
 // The same with 4 bytes per lane.
 __device__ __forceinline__ void load4_to_lds(const i32x4& buffer, uint32_t offset, uint32_t ahead, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dword %0, %2, %3 offen lds"
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %0, %2, %3 offen lds"
                : : "v"(offset), "s"(dst), "s"(buffer), "s"(ahead) : "memory", "m0");
 }
 
