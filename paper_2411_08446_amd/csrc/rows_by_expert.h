@@ -210,8 +210,9 @@ __device__ __forceinline__ float activate(float v, int act) {
 __device__ __forceinline__ float activation_slope(float v, int act) {
   if (act == LSHMOE_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
   if (act == LSHMOE_ACT_GELU) {
-    const NormalTail n = normal_tail(fminf(fabsf(v), 64.0f));
-    return fmaf(v, n.density, v < 0.0f ? n.beyond : 1.0f - n.beyond);
+    const float u = fabsf(v) > 64.0f ? 64.0f : fabsf(v);        // as above; a NaN stays one
+    const NormalTail n = normal_tail(u);
+    return fmaf(copysignf(u, v), n.density, v < 0.0f ? n.beyond : 1.0f - n.beyond);
   }
   return 1.0f;
 }

@@ -239,6 +239,21 @@ def test_what_is_not_finite_stays_with_its_rows(dtype):
     assert torch.isnan(b[2][1].float()).all() and torch.isnan(b[3][1].float()).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+def test_slope_where_the_layer_below_is_infinite(act, dtype):
+    """The activations' slopes are 1 at +inf and 0 at -inf: the gradient there is the product itself, and 0."""
+    counts, d_in, d_out = [37, 50, 41], 72, 88
+    rows, E, filled, dev, ref = _inputs(counts, 0, d_in, d_out, dtype, 13)
+    pre = torch.randn(rows, d_in, generator=torch.Generator().manual_seed(14)).cuda().to(DT[dtype])
+    pre[::3, ::5], pre[1::3, 1::5] = float("inf"), float("-inf")
+    product, got = _blank(rows, d_in, dtype=dtype), _blank(rows, d_in, dtype=dtype)
+    lsh.lshmoe_expert_backward_input(dev["g"], dev["w"], dev["off"], product)
+    lsh.lshmoe_expert_backward_input(dev["g"], dev["w"], dev["off"], got, ACT[act], pre)
+    assert torch.equal(got[::3, ::5], product[::3, ::5])
+    assert (got[1::3, 1::5] == 0).all() and torch.isfinite(got.float()).all()
+
+
 def test_offsets_out_of_range_stay_in_bounds():
     """Offsets beyond the rows count as the nearest row; nothing outside the buffers is touched."""
     rows, d_in, d_out, E = 40, 64, 64, 3
