@@ -76,7 +76,7 @@ typedef enum {
 typedef enum {
   LSHMOE_F32 = 0,
   LSHMOE_BF16 = 1,
-  LSHMOE_DTYPE_INT_RANGE_ = 0x7fffffff /* not a dtype: makes every int a representable value, so that an unknown
+  LSHMOE_DTYPE_INT_RANGE_ = -0x7fffffff - 1 /* not a dtype: makes every int a representable value, so that an unknown
                                           code from a caller is an error return (LSHMOE_ERR_UNSUPPORTED), never
                                           undefined behaviour inside the library */
 } lshmoe_dtype;
@@ -100,7 +100,7 @@ typedef enum {
   LSHMOE_ACT_NONE = 0,
   LSHMOE_ACT_RELU = 1,        /* max(v, 0); slope 0 at 0                                           */
   LSHMOE_ACT_GELU = 2,        /* v * Phi(v), Phi the normal distribution function (no approximation) */
-  LSHMOE_ACT_INT_RANGE_ = 0x7fffffff /* not an activation: makes every int a representable value, as for lshmoe_dtype */
+  LSHMOE_ACT_INT_RANGE_ = -0x7fffffff - 1 /* not an activation: makes every int a representable value, as for lshmoe_dtype */
 } lshmoe_activation;
 
 /* Static, never-freed name of a status code. */
