@@ -264,7 +264,8 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void weight_grad_kernel(const ch
                                                                         char* __restrict__ grad_bias, float4* partial,
                                                                         float* partial_sums, int slots) {
   const int ptiles = (d_in + BP - 1) / BP, qtiles = (d_out + BQ - 1) / BQ;
-  const RowParts parts(offsets, E, rows, part_rows(rows_of(offsets, E - 1, rows).hi, ptiles * qtiles, PARTS));
+  // (without slots no expert is cut, whatever the offsets are)
+  const RowParts parts(offsets, E, rows, slots == 0 ? max(rows, kLeastPart) : part_rows(rows_of(offsets, E - 1, rows).hi, ptiles * qtiles, PARTS));
   const WeightGradJob<DT, TILE, BP, BQ> job = {grad_out, x, grad_w, grad_bias, partial, partial_sums, d_in, d_out, ptiles, qtiles,
                                                slots, parts};
   // an XCD's tiles are consecutive ones with an eighth of the work
@@ -361,7 +362,6 @@ hipError_t input_grad(const void* grad_out, const void* w, const int32_t* offset
   return input_grad_on_tiles<DT, Small>(grad_out, w, offsets, rows, d_in, d_out, E, act, pre, grad_x, stream);
 }
 
-
 template <typename DT> struct WeightGradPlan {
   typedef WeightGradShape<DT> S;
   typedef Tile<DT, DT, true, true, S::BP, S::BQ, S::WP, S::WQ> TILE;
@@ -372,7 +372,7 @@ template <typename DT> struct WeightGradPlan {
 
   WeightGradPlan(int64_t rows, int d_in, int d_out) {
     tiles = (uint64_t)((d_in + S::BP - 1) / S::BP) * ((d_out + S::BQ - 1) / S::BQ);
-    cut = rows > kLeastPart;
+    cut = rows > kLeastPart && tiles < S::PARTS;          // with as many tiles a part is all rows
     slots = cut ? part_slots(rows, tiles, S::PARTS) : 0;
     off_sums = slots * tiles * S::BP * S::BQ * 4;
     total_bytes = off_sums + slots * tiles * TILE::TQ * TILE::kThreads * 4;

@@ -202,6 +202,21 @@ def test_the_workspace_ends_where_it_says():
         assert bool((ws[need:] == 0xA5).all())
 
 
+@pytest.mark.parametrize("d_in,d_out,dtype", [(4096, 4096, "bf16"), (4104, 4120, "bf16"), (4096, 8200, "f32")])
+def test_weights_of_many_tiles_need_no_workspace(d_in, d_out, dtype):
+    """As many tiles of an expert as workgroups: no expert is cut, whatever its rows."""
+    counts = [1500, 0, 20]
+    assert lsh.lshmoe_expert_workspace_bytes(sum(counts), d_in, d_out, len(counts), _code(dtype)) == 0
+    assert lsh.lshmoe_expert_workspace_bytes(1 << 20, d_in, d_out, len(counts), _code(dtype)) == 0
+    rows, E, x, g, w, b, off = _make(counts, 5, d_in, d_out, dtype, 15)
+    gw = _blank(E, d_out, d_in, dtype=dtype)
+    lsh.lshmoe_expert_backward_weight(g, x, off, gw, None, torch.empty(0, dtype=torch.uint8, device="cuda"))
+    o = _offsets(counts)
+    for e in range(E):
+        lo, hi = o[e], o[e + 1]
+        _check(gw[e], g[lo:hi].double().t().contiguous(), x[lo:hi].double(), hi - lo, dtype, "grad_w of expert %d" % e)
+
+
 @pytest.mark.parametrize("d_in", [128, 160, 256, 384, 1024])
 def test_mx4_over_tiles_and_beside_them(d_in):
     """Whole and half chunks of 4-bit numbers, and rows that the tiles do not take (160)."""
