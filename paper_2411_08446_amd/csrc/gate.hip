@@ -23,16 +23,6 @@ __device__ __forceinline__ uint32_t order_of(float v) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// The value of a lane of the other half of 2 M lanes, where the M lanes of each half hold the same: lane ^ M, or a lane mirrored in 8
-// or 16, which moves within the vector unit.  Lanes 16 and 32 apart go through LDS's crossbar.
-template <int M> __device__ __forceinline__ uint32_t other_half(uint32_t v) {
-  constexpr int kQuad1 = 0xb1, kQuad2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;   // lanes 1 0 3 2; 2 3 0 1; 7 - i; 15 - i
-  constexpr int kControl = M == 1 ? kQuad1 : M == 2 ? kQuad2 : M == 4 ? kHalfMirror : kMirror;
-  if (M > 8) return (uint32_t)__shfl_xor((int)v, M, 64);
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kControl, 0xf, 0xf, true);
-}
-template <int M> __device__ __forceinline__ float other_half(float v) { return __uint_as_float(other_half<M>(__float_as_uint(v))); }
-
 // f(std::integral_constant<int, M>) for M = 1, 2, .. below G.
 template <int G, int M = 1, typename F> __device__ __forceinline__ void over_halves(F&& f) {
   if constexpr (M < G) {
