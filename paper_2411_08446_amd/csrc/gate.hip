@@ -4,7 +4,9 @@
 // 4 (i + G c) + j, so that a token's row comes in whole 16-byte pieces.  Choosing is k rounds of an arg-max over the lanes' own best candidates: the
 // comparison is on (value, lower index), so a round's winner does not depend on the order of the exchanges.
 //
-// The bound is the read of the logits (and in the backward pass the write of their gradient): 4 E bytes per token.
+// The floor is the read of the logits (and in the backward pass the write of their gradient): 4 E bytes per token.  65536 tokens of 64
+// experts, k = 2: 8.8 us, 8.0 backward with the softmax over all; k rounds of exchanges are a chain that a lane waits for (k = 8 of 256
+// experts: 38 us, 1.8 TB/s), hence 16 lanes to a token, whose exchanges stay within the vector unit (64 lanes: 106 us).
 #include <type_traits>
 
 #include "kernels.h"

@@ -12,6 +12,12 @@
 // A wave spreads its loads between its products: a chunk's loads all at once fill the address units' queue, and the
 // products behind them wait.  The chunks of all tiles of a workgroup are one stream: while a tile's results are
 // stored, the first chunks of the next are on their way.
+//
+// Measured.  131072 rows of 32 experts, 4096 -> 4096 columns of bf16: 3494 us, 1.26 PFLOP/s; bound by the matrix cores (busy two thirds
+// of the time; the loop's barriers and the clock on real data take the rest).  1024 -> 4096 columns of 64 experts with values
+// kept before the activation: 1325 us, 0.83 PFLOP/s; a tile's results are as many bytes as its operands there, and their
+// stores, 14 us to a round of tiles, do not overlap with products.  The same in 4 bits: 1552 us, 2.8 PFLOP/s; 566 us for 1024 -> 4096
+// columns.  binary32, 15011 rows of 6 experts, 1000 -> 1500 columns: 399 us, 113 TFLOP/s.
 #pragma once
 
 #include <type_traits>
@@ -533,7 +539,8 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   // ---- results: lanes and memory.  Of the 32 x 32 results of tiles t, u a lane has q = r = lane % 32 and, h = lane / 32, p = 8 j + 4 h
   // + 0 .. 3 for j = 0 .. 3.  Three exchanges between lanes make that 16 bytes of consecutive p to a lane and whole lines of 128
   // bytes of 8 rows to an instruction: a group, 128 bytes of p (one tile of binary32, two of bf16) by 32 q, is four pieces
-  // to a lane, of q = 8 i + lane % 8.  (64 bytes of 16 rows: 13 % more time at K = 1024 with two results stored.)
+  // to a lane, of q = 8 i + lane % 8.  (64 bytes of 16 rows: 1578 us in place of 1326 at K = 1024
+  // with two results stored.)
   static constexpr int kItemsPerWord = 4 / ItemSize<DT>::value;
   static constexpr int kGroupTiles = kItemsPerWord, kGroups = TP / kGroupTiles;
   static constexpr int kStores = kGroups * TQ * 4;
