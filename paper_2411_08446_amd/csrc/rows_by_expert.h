@@ -199,10 +199,11 @@ __device__ __forceinline__ NormalTail normal_tail(float u) {
 }
 
 __device__ __forceinline__ float activate(float v, int act) {
-  if (act == LSHMOE_ACT_RELU) return v < 0.0f ? 0.0f : v;
+  const float above = __builtin_elementwise_maximum(v, 0.0f);     // one instruction, a NaN stays one
+  if (act == LSHMOE_ACT_RELU) return above;
   if (act == LSHMOE_ACT_GELU) {
     const float u = fminf(fabsf(v), 64.0f);       // infinities: 64 is as good
-    return fmaf(-u, normal_tail(u).beyond, v < 0.0f ? 0.0f : v);
+    return fmaf(-u, normal_tail(u).beyond, above);
   }
   return v;
 }

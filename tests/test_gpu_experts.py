@@ -254,6 +254,27 @@ def test_slope_where_the_layer_below_is_infinite(act, dtype):
     assert (got[1::3, 1::5] == 0).all() and torch.isfinite(got.float()).all()
 
 
+@pytest.mark.parametrize("counts", [[5, 3], [300, 200]])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+def test_activations_of_what_is_not_finite(act, dtype, counts):
+    """max(v, 0) and v Phi(v) at +inf, -inf and NaN of either sign, through the bias, on the few-row kernel and on tiles."""
+    rows, E, d_in, d_out = sum(counts), 2, 64, 128
+    x, w = torch.zeros(rows, d_in, device="cuda", dtype=DT[dtype]), torch.zeros(E, d_out, d_in, device="cuda", dtype=DT[dtype])
+    nan = float("nan")
+    bias = torch.tensor([float("inf"), float("-inf"), nan, -nan, 2.0, -2.0, 0.0, -0.0] * 16, device="cuda", dtype=DT[dtype]).repeat(E, 1)
+    out, pre = _blank(rows, d_out, dtype=dtype), _blank(rows, d_out, dtype=dtype)
+    lsh.lshmoe_expert_forward(x, w, bias, torch.tensor(_offsets(counts), dtype=torch.int32, device="cuda"), out, act=ACT[act], pre=pre)
+    got = out.float().cpu().view(rows, 16, 8)
+    assert (got[..., 0] == float("inf")).all() and (got[..., 1] == 0).all() and torch.isnan(got[..., 2:4]).all()
+    assert (got[..., 6:] == 0).all()
+    assert torch.isnan(pre.float().cpu().view(rows, 16, 8)[..., 2:4]).all()
+    want = (2.0, 0.0) if act == "relu" else (1.9544997, -0.0455003)
+    # v Phi(v) is good to 2 * 2^-21, and is rounded
+    for i in range(2):
+        assert (got[..., 4 + i] - want[i]).abs().max() <= 2.0 ** -20 + HALF_STEP[dtype] * 2.0
+
+
 def test_offsets_out_of_range_stay_in_bounds():
     """Offsets beyond the rows count as the nearest row; nothing outside the buffers is touched."""
     rows, d_in, d_out, E = 40, 64, 64, 3
