@@ -15,8 +15,8 @@
 //
 // Measured.  131072 rows of 32 experts, 4096 -> 4096 columns of bf16: 3494 us, 1.26 PFLOP/s; bound by the matrix cores (busy two thirds
 // of the time; the loop's barriers and the clock on real data take the rest).  1024 -> 4096 columns of 64 experts with values
-// kept before the activation: 1325 us, 0.83 PFLOP/s; a tile's results are as many bytes as its operands there, and their
-// stores, 14 us to a round of tiles, do not overlap with products.  The same in 4 bits: 1552 us, 2.8 PFLOP/s; 566 us for 1024 -> 4096
+// kept before the activation: 1264 to 1325 us, 0.83 to 0.87 PFLOP/s; a tile's results are as many bytes as its operands there, and their
+// stores, 14 us to a round of tiles, do not overlap with products.  The same in 4 bits: 1433 us, 3.1 PFLOP/s; 416 us for 1024 -> 4096
 // columns.  binary32, 15011 rows of 6 experts, 1000 -> 1500 columns: 399 us, 113 TFLOP/s.
 #pragma once
 
@@ -637,9 +637,10 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     for (int i = 0; i < 4; ++i) x.v[i % 2 * 2 + i / 2] = (u32x4){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
     return x;
   }
-  __device__ __forceinline__ static void put(const Lines& l, int g, int u, const Pieces& x) {
+  // STREAM: the lines are not kept in the caches.
+  template <bool STREAM = false> __device__ __forceinline__ static void put(const Lines& l, int g, int u, const Pieces& x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b128(x.v[i], l.buffer, (int)piece_at(l, g, u, i), 0, 0);
+    for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b128(x.v[i], l.buffer, (int)piece_at(l, g, u, i), 0, STREAM ? 2 : 0);
   }
   __device__ __forceinline__ static Pieces get(const Lines& l, int g, int u) {
     Pieces x;
@@ -761,7 +762,10 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
         if (KEEP) TILE::put(k, g, u, TILE::pack(v));
 #pragma unroll
         for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] = activate(v[i], ACT);
-        TILE::put(o, g, u, TILE::pack(v));
+        // Streaming stores of 4-bit products, which write many times what they read: 1024 -> 4096 columns, 131072 rows of 64 experts
+        // 573 -> 416 us, 16384 rows of 32 61 -> 60, 2048 of 16 17 -> 15; a kernel that reads the results next takes as
+        // much longer as they gain, or less.  bf16 products: 1264 and 1277 us, 1027 and 1031, 180 and 175.
+        TILE::template put<kScaled>(o, g, u, TILE::pack(v));
       }
     }
   }
