@@ -38,6 +38,7 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
             min(BP, d_in - p0), nq, d_out, TILE::OpP::kChunk, expert, first, p0};
   }
   __device__ __forceinline__ bool sums(const Place&) const { return false; }
+  __device__ __forceinline__ bool twice() const { return false; }
   template <int ACT> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
     const int64_t first = ((int64_t)at.first * d_in + at.p0) * kItem;
     const typename TILE::Lines o = TILE::lines(grad_x + first, (uint32_t)d_in * kItem, at.nq, at.np);
@@ -171,6 +172,7 @@ template <typename DT, typename TILE, int BP, int BQ> struct WeightGradJob {
             min(BQ, d_out - q0), t.v[3], e, p0, q0, t.v[1], t.v[4]};
   }
   __device__ __forceinline__ bool sums(const Place& at) const { return grad_bias != nullptr && at.p0 == 0; }
+  __device__ __forceinline__ bool twice() const { return false; }
   __device__ __forceinline__ float4* partial_at(int slot, int tile, int i, int thread) const {
     return partial + (((int64_t)slot * ptiles * qtiles + tile) * (TILE::TP * TILE::TQ * 4) + i) * TILE::kThreads + thread;
   }

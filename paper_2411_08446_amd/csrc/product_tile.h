@@ -316,7 +316,7 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   // everything of chunk c + 1, two or three to a half step.
   template <bool SUMS, bool FIRST, bool LAST, typename SwitchP, typename SwitchQ>
   __device__ __forceinline__ void chunk(const FragP& fp, const FragQ& fq, Feed& f, SwitchP&& switch_p, SwitchQ&& switch_q,
-                                        bool stores) {
+                                        int stores) {
     lds_char* const now_p = f.lds + f.slot_p * OpP::kBytes;
     lds_char* const now_q = f.lds + kAtQ + f.slot_q * OpQ::kBytes;
     const int slot_next = f.slot_p == kRingP - 1 ? 0 : f.slot_p + 1, slot_free = f.slot_p == 0 ? kRingP - 1 : f.slot_p - 1;
@@ -342,7 +342,8 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
         // free, the next one may be read.
         constexpr int kUnderWay = kScaled ? 0 : 4;
         if (FIRST) {
-          if (stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kUnderWay + kStores) : "memory");
+          if (!kScaled && stores == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kScaled ? 0 : kUnderWay + 2 * kStores) : "memory");
+          else if (stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kUnderWay + kStores) : "memory");
           else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kUnderWay) : "memory");
         } else {
           asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kUnderWay) : "memory");
@@ -434,7 +435,7 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   // All chunks of a tile.
   template <bool SUMS, typename SwitchP, typename SwitchQ>
   __device__ __forceinline__ void products(const FragP& fp, const FragQ& fq, Feed& f, SwitchP&& switch_p, SwitchQ&& switch_q,
-                                           int chunks, bool stores) {
+                                           int chunks, int stores) {
     if (chunks == 1) {
       chunk<SUMS, true, true>(fp, fq, f, switch_p, switch_q, stores);
       return;
@@ -445,7 +446,8 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
   }
 
   // The tiles n, n + step, .. below end.  JOB: entry(n) says which tile n is, each lane of another one; place(entry) gives a
-  // tile's operands and where its results go; finish(place, tile) stores them, with kStores stores to a wave or more.
+  // tile's operands and where its results go; finish(place, tile) stores them, with kStores stores to a wave or more, or
+  // twice that where job.twice().
   // Lane i of a wave has the entry of the tile i steps on: looked up one by one between the products, they cost
   // 3 of a tile's 40 us at K = 1024.
   template <typename JOB> __device__ __forceinline__ void run(const JOB& job, int n, int end, int step) {
@@ -513,7 +515,7 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
     load_q(1);
-    bool stores = false;
+    int stores = 0;          // of the tile before, in units of kStores
     for (;;) {
       // the first fragments and scales (again behind a finished tile: they would take registers that its results need)
 #pragma unroll
@@ -529,7 +531,7 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
       if (JOB::kSums && job.sums(here)) products<JOB::kSums>(fp, fq, f, switch_p, switch_q, here.chunks(), stores);
       else products<false>(fp, fq, f, switch_p, switch_q, here.chunks(), stores);
       job.finish(here, *this);
-      stores = true;
+      stores = job.twice() ? 2 : 1;
       if (++at == count) break;
       here = place(at);
     }
@@ -739,6 +741,7 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
             TILE::OpP::kChunk, expert, first, p0};
   }
   __device__ __forceinline__ bool sums(const Place&) const { return false; }
+  __device__ __forceinline__ bool twice() const { return !kScaled && pre != nullptr; }
   template <int ACT, bool KEEP> __device__ __forceinline__ void store(const Place& at, const TILE& tile) const {
     const int64_t first = ((int64_t)at.first * d_out + at.p0) * kItem;
     const typename TILE::Lines o = TILE::lines(out + first, (uint32_t)d_out * kItem, at.nq, at.np);
