@@ -13,11 +13,12 @@
 // products behind them wait.  The chunks of all tiles of a workgroup are one stream: while a tile's results are
 // stored, the first chunks of the next are on their way.
 //
-// Measured.  131072 rows of 32 experts, 4096 -> 4096 columns of bf16: 3494 us, 1.26 PFLOP/s; bound by the matrix cores (busy two thirds
-// of the time; the loop's barriers and the clock on real data take the rest).  1024 -> 4096 columns of 64 experts with values
-// kept before the activation: 1264 to 1325 us, 0.83 to 0.87 PFLOP/s; a tile's results are as many bytes as its operands there, and their
-// stores, 14 us to a round of tiles, do not overlap with products.  The same in 4 bits: 1433 us, 3.1 PFLOP/s; 416 us for 1024 -> 4096
-// columns.  binary32, 15011 rows of 6 experts, 1000 -> 1500 columns: 399 us, 113 TFLOP/s.
+// Measured.  131072 rows of 32 experts, 4096 -> 4096 columns of bf16: 3365 to 3494 us, 1.26 to 1.31 PFLOP/s; bound by the matrix cores
+// (busy two thirds of the time; the loop's barriers and the clock on real data take the rest).  1024 -> 4096 columns of 64
+// experts with values kept before the activation: 1276 to 1325 us, 0.83 to 0.86 PFLOP/s; a tile's results are as many bytes
+// as its operands there, and their stores, 14 us to a round of tiles, hardly overlap with products: loads that are issued behind
+// them count as done behind them.  The same in 4 bits: 1433 us, 3.1 PFLOP/s; 416 us for 1024 -> 4096 columns.  binary32, 15011
+// rows of 6 experts, 1000 -> 1500 columns: 393 us, 115 TFLOP/s.
 #pragma once
 
 #include <type_traits>
@@ -341,6 +342,7 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
         // finished tile's stores may be under way).  Behind the barrier that is so for all waves: this chunk's slots are
         // free, the next one may be read.
         constexpr int kUnderWay = kScaled ? 0 : 4;
+        static_assert(kScaled || kUnderWay + 2 * kStores < 64, "what a wait can name");
         if (FIRST) {
           if (!kScaled && stores == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kScaled ? 0 : kUnderWay + 2 * kStores) : "memory");
           else if (stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kUnderWay + kStores) : "memory");
