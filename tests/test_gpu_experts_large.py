@@ -217,6 +217,37 @@ def test_weights_of_many_tiles_need_no_workspace(d_in, d_out, dtype):
         _check(gw[e], g[lo:hi].double().t().contiguous(), x[lo:hi].double(), hi - lo, dtype, "grad_w of expert %d" % e)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_longest_rows(dtype):
+    """Rows of 16 bytes less than 8 MiB, more than 2 GiB of them to an expert, as d_in of the forward product and the weight gradient
+    and as d_out of the input gradient; on tiles and (the second call, with few rows) without."""
+    piece = 8 if dtype == "bf16" else 4
+    d = (8 << 20) * piece // 16 - piece
+    for counts in ([300, 7], [5, 2]):
+        rows, E, long, short, w, b, off = _make(counts, 2, d, piece, dtype, 16)      # long [rows, d], short [rows, piece], w [E, piece, d]
+        o = _offsets(counts)
+        out, gw, gx = _blank(rows, piece, dtype=dtype), _blank(E, piece, d, dtype=dtype), _blank(rows, piece, dtype=dtype)
+        wt = w.transpose(1, 2).contiguous()                                         # [E, d, piece]: from `piece` to d columns
+        lsh.lshmoe_expert_forward(long, w, b, off, out)
+        lsh.lshmoe_expert_backward_input(long, wt, off, gx)
+        lsh.lshmoe_expert_backward_weight(short, long, off, gw, None, _workspace(rows, d, piece, E, dtype))
+        assert (out[o[-1]:] == 7.0).all() and (gx[o[-1]:] == 7.0).all()
+        for e in range(E):
+            lo, hi = o[e], o[e + 1]
+            xe, we = long[lo:hi].double(), wt[e].double()
+            _check(out[lo:hi], xe, we, d, dtype, "out of expert %d" % e, b[e].double())
+            _check(gx[lo:hi], xe, we, d, dtype, "grad_x of expert %d" % e)
+            _check(gw[e], short[lo:hi].double().t().contiguous(), xe, hi - lo, dtype, "grad_w of expert %d" % e)
+            del xe, we
+
+
+def test_as_many_experts_as_there_may_be():
+    """4096 experts of 0 to 40 rows, most of the sizes at once."""
+    gen = torch.Generator().manual_seed(17)
+    counts = torch.randint(0, 41, (4096,), generator=gen).tolist()
+    _all_three(counts, 3, 64, 40, "bf16", 18, experts=[0, 1, 63, 64, 65, 2047, 2048, 4094, 4095])
+
+
 @pytest.mark.parametrize("d_in", [128, 160, 256, 384, 1024])
 def test_mx4_over_tiles_and_beside_them(d_in):
     """Whole and half chunks of 4-bit numbers, and rows that the tiles do not take (160)."""
