@@ -808,16 +808,16 @@ struct Large { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, kPerUnit
 struct Small { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, kPerUnit = 2; };
 
 // Small tiles where a call has at most 128 rows per expert on average or fewer large tiles than compute units (1024 -> 4096 columns
-// of 16 experts: 2048 rows 28.7 us and 34 on large tiles, 4096 rows 43.3 and 39.5; 4 bits 16.2 and 19.7, 23.6 and 21.8;
-// 512 -> 512 columns of 8 experts, 16384 rows, 4 bits: 12.0 and 15.2; with work enough large ones are 20 % faster).
+// of 16 experts: 2048 rows 28.7 us and 34 on large tiles, 4096 rows 43.3 and 39.5; 4 bits 14.5 and 17.9, 23.6 and 21.1;
+// 512 -> 512 columns of 8 experts, 16384 rows, 4 bits: 10.9 and 14.1; with work enough large ones are 20 % faster).
 inline bool small_tiles(int64_t rows, int E, int columns) {
   return rows <= 128 * (int64_t)E || (uint64_t)most_row_tiles(rows, E, Large::BQ) * ((columns + Large::BP - 1) / Large::BP) < (uint64_t)kUnits;
 }
 
 // Waves that read the weights for themselves (product_direct.h) where a call has at most `few` rows per expert on average and no more
 // small tiles than run at a time (16 experts, 74 rows: 768 -> 2048 columns 13.1 and 13.9 us on tiles, 2048 -> 768 13.1 and
-// 22.9; 4 bits 8.9 and 9.3, 9.4 and 11.6; 256 rows 15.6 and 13.8; 64 experts, 256 rows, 1024 -> 4096 columns 100 and 96, 4 bits
-// 47 and 35).
+// 22.9; 4 bits 9.1 and 10.5, 9.0 and 11.6; 256 rows 15.6 and 13.8; 64 experts, 256 rows, 1024 -> 4096 columns 100 and 96, 4 bits
+// 47 and 33).
 inline bool few_rows(int64_t rows, int E, int columns, int few) {
   return rows <= few * (int64_t)E && (uint64_t)most_row_tiles(rows, E, Small::BQ) * ((columns + Small::BP - 1) / Small::BP) <=
                                          (uint64_t)kUnits * Small::kPerUnit;
