@@ -66,7 +66,7 @@ template <typename DT, typename TILE, int BP, int BQ> struct InputGradJob {
             float z[kElems];
             TILE::spread(x[g][u], z);
 #pragma unroll
-            for (int i = 0; i < kElems; ++i) v[i] *= activation_slope(z[i], ACT);
+            for (int i = 0; i < kElems; ++i) v[i] *= activation_slope<DT>(z[i], ACT);
           }
           y[g][u] = TILE::pack(v);
         }

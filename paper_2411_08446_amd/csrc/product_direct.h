@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void direct_kernel(const char* __restrict__ x,
       for (int j = 0; j < 4; ++j) v[j] = acc[u][j] + add[j];
       if (pre) store4(pre + at, v);
   #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = activate(v[j], act);
+      for (int j = 0; j < 4; ++j) v[j] = activate<DT>(v[j], act);
       store4(out + at, v);
     }
   }

@@ -766,7 +766,7 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
         for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] += TILE::four(b[g * TILE::kGroupTiles + i / 16], i % 16);
         if (KEEP) TILE::put(k, g, u, TILE::pack(v));
 #pragma unroll
-        for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] = activate(v[i], ACT);
+        for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] = activate<DT>(v[i], ACT);
         // Streaming stores of 4-bit products, which write many times what they read: 1024 -> 4096 columns, 131072 rows of 64 experts
         // 573 -> 416 us, 16384 rows of 32 61 -> 60, 2048 of 16 17 -> 15; a kernel that reads the results next takes as
         // much longer as they gain, or less.  bf16 products: 1264 and 1277 us, 1027 and 1031, 180 and 175.
