@@ -38,8 +38,11 @@ template <int G> __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// The larger one; a NaN stays one.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 template <int G> __device__ __forceinline__ float group_max(float v) {
-  over_halves<G>([&](auto m) { v = fmaxf(v, other_half<decltype(m)::value>(v)); });
+  over_halves<G>([&](auto m) { v = larger(v, other_half<decltype(m)::value>(v)); });
   return v;
 }
 
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(kGateThreads) void gate_topk_backward_kernel(const 
   if (full) {
     float top = v[0], sum = 0.0f;
 #pragma unroll
-    for (int i = 1; i < 4 * C; ++i) top = fmaxf(top, v[i]);
+    for (int i = 1; i < 4 * C; ++i) top = larger(top, v[i]);
     top = group_max<G>(top);
 #pragma unroll
     for (int i = 0; i < 4 * C; ++i) {
