@@ -438,7 +438,7 @@ lshmoe_status lshmoe_gate_topk(const float* logits, int64_t T, int32_t E, int32_
  *     grad_logits[t][expert[t][j]] = w_j (g_j - h), 0 for the experts that were not chosen;
  * with LSHMOE_FLAG_GATE_FULL_SOFTMAX, p the softmax over all E logits (computed again from them):
  *     grad_logits[t][e] = p_e ((g_j if e is expert[t][j], else 0) - h).
- * A token all of whose logits are -inf gets a gradient of 0.  A token that has a NaN or +inf among the logits summed over gets NaN
+ * A token all of whose logits are -inf gets a gradient of 0, whatever grad_gate_weight holds for it.  A token that has a NaN or +inf among the logits summed over gets NaN
  * for all of them, as its weights are.
  *
  *   logits           [T, E]  in   binary32; may be NULL without LSHMOE_FLAG_GATE_FULL_SOFTMAX (not read then)

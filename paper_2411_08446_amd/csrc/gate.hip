@@ -141,12 +141,17 @@ __global__ __launch_bounds__(kGateThreads) void gate_topk_backward_kernel(const 
   float v[4 * C];
   if (full) load_logits<G, C, VEC>(logits + (live ? t : 0) * (uint64_t)E, lane, E, v);
   float mean = 0.0f;
-  for (int j = 0; j < k; ++j) mean = fmaf(weight[a0 + j], grad_weight[a0 + j], mean);
+  bool any = false;        // a token all of whose experts are masked has only weights of 0 (the largest logit's is 1 / E at least)
+  for (int j = 0; j < k; ++j) {
+    mean = fmaf(weight[a0 + j], grad_weight[a0 + j], mean);
+    any |= weight[a0 + j] != 0.0f;
+  }
   float out[4 * C] = {};
   for (int j = 0; j < k; ++j) {
     const int e = min((uint32_t)expert[a0 + j], (uint32_t)(E - 1));
     const float g = grad_weight[a0 + j];
-    const float term = full ? g : weight[a0 + j] * (g - mean);
+    // (whatever the gradients of its weights are: behind a masked token there may be rows that hold anything)
+    const float term = full ? g : any ? weight[a0 + j] * (g - mean) : 0.0f;
 #pragma unroll
     for (int i = 0; i < 4 * C; ++i)
       if (4 * (lane + G * (i / 4)) + i % 4 == e) out[i] += term;

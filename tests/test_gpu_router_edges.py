@@ -55,3 +55,32 @@ def test_nan_among_the_logits_reaches_the_gradient(E):
         chosen[ids[t]] = True
         assert torch.isnan(got[t][chosen]).all() and (got[t][~chosen] == 0.0).all(), "token %d" % t
     assert (got[5] == 0.0).all() and torch.isfinite(got[6:]).all()
+
+
+@pytest.mark.parametrize("full", [False, True])
+@pytest.mark.parametrize("E", [3, 8, 60, 256, 1000])
+def test_a_token_without_experts_gets_zeros_whatever_its_gradient_is(E, full):
+    """Its weights are 0, and the rows behind them may hold anything: infinities and NaN of their gradients end there."""
+    k = min(4, E)
+    gen = torch.Generator().manual_seed(E)
+    logits = torch.randn(5, E, generator=gen)
+    logits[1:4] = -INF
+    g = torch.randn(5, k, generator=gen)
+    g[1], g[2, 0], g[3, k - 1] = NAN, INF, -INF
+    flags = lsh.LSHMOE_FLAG_GATE_FULL_SOFTMAX if full else 0
+    lt = logits.cuda()
+    ids, w = _forward(lt, k, flags)
+    got = _backward(lt if full else None, ids, w, g.cuda(), E, flags)
+    assert (w.cpu()[1:4] == 0.0).all() and (got[1:4] == 0.0).all()
+    assert torch.isfinite(got[0]).all() and torch.isfinite(got[4]).all() and (got[0] != 0.0).any()
+
+
+def test_a_gradient_that_is_not_finite_reaches_the_token_whose_weights_are_not_zero():
+    logits = torch.tensor([[1.0, -INF, 0.0, -INF, 2.0]] * 2)
+    g = torch.tensor([[1.0, NAN, 0.5], [1.0, 2.0, INF]])
+    for flags in (0, lsh.LSHMOE_FLAG_GATE_FULL_SOFTMAX):
+        lt = logits.cuda()
+        ids, w = _forward(lt, 3, flags)
+        got = _backward(lt, ids, w, g.cuda(), 5, flags)
+        assert ids.tolist() == [[4, 0, 2]] * 2
+        assert torch.isnan(got[0, [4, 0, 2]]).all() and not torch.isfinite(got[1, [4, 0, 2]]).any()
