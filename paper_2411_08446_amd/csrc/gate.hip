@@ -1,6 +1,6 @@
 // Router: the k experts of a token from the logits of its gate, with their weights, and the gradient of the logits.
 //
-// G lanes share a token (G a power of two, up to 16 pieces of 4 logits to a lane, c = 0 .. C - 1); lane i of them holds the logits
+// G lanes share a token (G a power of two, up to C = 4 pieces of 4 logits to a lane, c = 0 .. C - 1); lane i of them holds the logits
 // 4 (i + G c) + j, so that a token's row comes in whole 16-byte pieces.  Choosing is k rounds of an arg-max over the lanes' own best candidates: the
 // comparison is on (value, lower index), so a round's winner does not depend on the order of the exchanges.
 //

@@ -13,12 +13,16 @@
 // products behind them wait.  The chunks of all tiles of a workgroup are one stream: while a tile's results are
 // stored, the first chunks of the next are on their way.
 //
-// Measured.  131072 rows of 32 experts, 4096 -> 4096 columns of bf16: 3365 to 3494 us, 1.26 to 1.31 PFLOP/s; bound by the matrix cores
-// (busy two thirds of the time; the loop's barriers and the clock on real data take the rest).  1024 -> 4096 columns of 64
-// experts with values kept before the activation: 1276 to 1325 us, 0.83 to 0.86 PFLOP/s; a tile's results are as many bytes
-// as its operands there, and their stores, 14 us to a round of tiles, hardly overlap with products: loads that are issued behind
-// them count as done behind them.  The same in 4 bits: 1433 us, 3.1 PFLOP/s; 416 us for 1024 -> 4096 columns.  binary32, 15011
-// rows of 6 experts, 1000 -> 1500 columns: 393 us, 115 TFLOP/s.
+// Measured, as many rows to every expert (no tile partly empty) where nothing else is said.  131072 rows of 32 experts, 4096 -> 4096
+// columns of bf16: 3334 to 3494 us, 1.26 to 1.32 PFLOP/s; bound by the matrix cores (busy two thirds of the time; the loop's
+// barriers and the clock on real data take the rest).  1024 -> 4096 columns of 64 experts with values kept before the
+// activation: 1267 to 1294 us with ReLU, 0.85 to 0.87 PFLOP/s, and 1361 to 1376 with GELU (ReLU, 1557 to 2667 rows to an expert:
+// 1314).  A tile's results are as many bytes as its operands there, and their stores, 14 us to a round of tiles, do not overlap
+// with products: the 256 x 256 forward kernels do not have registers enough (bf16 keeps 17 words of a lane in scratch memory, two of the
+// table of tiles among them, 4 bits 4 to 8), and the wait for what is fetched from there, in front of the next tile, is one for the
+// stores too, since operations count as done in their order.  4 bits: 4096 -> 4096 columns 1433 to 1457 us, 3.0 to 3.1 PFLOP/s;
+// 1024 -> 4096 columns 418 us, with 1557 to 2667 rows to an expert 445, and 553 behind the quantisation of rows that are new each time.
+// binary32, 15011 rows of 6 experts, 1000 -> 1500 columns, GELU: 393 to 402 us, 112 to 115 TFLOP/s.
 #pragma once
 
 #include <type_traits>
@@ -339,8 +343,9 @@ template <typename OT, typename DT, bool P_COLUMNS, bool Q_COLUMNS, int BP, int 
       constexpr bool kEnd = i == 2 * kSteps - 1;
       if (kEnd) {
         // The last fragments of this chunk are in registers, this wave's share of the next one has landed (P's of the one after it and a
-        // finished tile's stores may be under way).  Behind the barrier that is so for all waves: this chunk's slots are
-        // free, the next one may be read.
+        // finished tile's stores may be under way, as far as this wait goes: in the kernels that fetch spilled registers in front
+        // of a tile the stores have ended there).  Behind the barrier that is so for all waves: this chunk's slots are free, the
+        // next one may be read.
         constexpr int kUnderWay = kScaled ? 0 : 4;
         static_assert(kScaled || kUnderWay + 2 * kStores < 64, "what a wait can name");
         if (FIRST) {
@@ -749,7 +754,7 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
     const typename TILE::Lines o = TILE::lines(out + first, (uint32_t)d_out * kItem, at.nq, at.np);
     const typename TILE::Lines k = TILE::lines((KEEP ? pre : out) + first, (uint32_t)d_out * kItem, at.nq, at.np);
     // all loads in front of the stores: operations count as done in their order, and a load behind a store would wait until
-    // that has reached memory
+    // that has reached memory (they wait for the next tile's first loads, which are in front of them)
     typename TILE::Fours b[TILE::TP] = {};
     if (bias) {
 #pragma unroll
@@ -767,8 +772,8 @@ template <typename OT, typename DT, typename TILE, int BP, int BQ> struct Forwar
         if (KEEP) TILE::put(k, g, u, TILE::pack(v));
 #pragma unroll
         for (int i = 0; i < 16 * TILE::kGroupTiles; ++i) v[i] = activate<DT>(v[i], ACT);
-        // Streaming stores of 4-bit products, which write many times what they read: 1024 -> 4096 columns, 131072 rows of 64 experts
-        // 573 -> 416 us, 16384 rows of 32 61 -> 60, 2048 of 16 17 -> 15; a kernel that reads the results next takes as
+        // Streaming stores of 4-bit products, which write many times what they read: 1024 -> 4096 columns, 131072 rows of 64 experts,
+        // 2048 each, 573 -> 416 us, 16384 rows of 32 61 -> 60, 2048 of 16 17 -> 15; a kernel that reads the results next takes as
         // much longer as they gain, or less.  bf16 products: 1264 and 1277 us, 1027 and 1031, 180 and 175.
         TILE::template put<kScaled>(o, g, u, TILE::pack(v));
       }
@@ -807,6 +812,8 @@ constexpr int kUnits = 256;   // compute units
 struct Large { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, kPerUnit = 1; };
 struct Small { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, kPerUnit = 2; };
 
+// Both rules go by the rows of the call's buffer: how many of them belong to experts is known to the device only.
+//
 // Small tiles where a call has at most 128 rows per expert on average or fewer large tiles than compute units (1024 -> 4096 columns
 // of 16 experts: 2048 rows 28.7 us and 34 on large tiles, 4096 rows 43.3 and 39.5; 4 bits 14.5 and 17.9, 23.6 and 21.1;
 // 512 -> 512 columns of 8 experts, 16384 rows, 4 bits: 10.9 and 14.1; with work enough large ones are 20 % faster).
